@@ -392,6 +392,124 @@ wnw_status_t wnw_attend_static(const void *kv_dev, int32_t n_tokens, int32_t pad
                                void *cuda_stream);
 wnw_status_t wnw_attend_static_status(int32_t device, void *cuda_stream, int32_t *timed_out_host);
 
+/* ---- Operators around a caller-owned, paged K/V store of eight bits -----------------------------------------------------
+ * For callers that keep K,V themselves, as wnw_attend_static's do, but of many sequences, growing token by token, in pages,
+ * and in a quarter of float's size.  None of the calls allocates, synchronises or keeps anything between calls; all queue
+ * their work on cuda_stream and may be captured into a graph.  Every index that a kernel takes from device memory (page
+ * ids, lengths, row starts) is checked there before it is used: what lies outside is skipped, and if the caller gives a
+ * status word, bits WNW_PAGES_* are set in it.  (The paper's footnote calls KV quantisation orthogonal to the method, and the
+ * position encoding is the caller's job: the calls stand beside the cache, and wnw_pages_read hands its inputs over.) */
+
+enum { WNW_DTYPE_BF16 = 0, WNW_DTYPE_FP16 = 1, WNW_DTYPE_FP32 = 2 };
+
+/* Rows of heads, one row per token: element (row, head, i) at dev[row * row_stride + head * head_stride + i].  Strides in
+ * elements, so slices of a fused projection's output can be given; dev on 16 bytes and both strides multiples of 16 bytes
+ * where not said otherwise. */
+typedef struct {
+  void *dev;
+  int64_t row_stride, head_stride;
+  int32_t n_heads;
+  int32_t reserved;
+} wnw_rows_t;
+
+/* Rotary positions with several axes (time, height, width; or time alone): a plan, filled by wnw_rotary_init or by hand, copied
+ * by the calls that take it.  Pair i of a head is the elements (i, i + n_pairs), or with neighbours = 1 (2i, 2i + 1); elements
+ * from 2 * n_pairs on are left as they are. */
+typedef struct {
+  int32_t n_pairs;          /* 1..128 */
+  int32_t n_axes;           /* 1..4 */
+  int32_t neighbours;
+  int32_t reserved;
+  double frequency[128];    /* radians a position, per pair */
+  uint8_t axis[128];        /* which axis turns the pair */
+} wnw_rotary_t;
+
+/* frequency[i] = base^(-i / n_pairs).  sections: HOST [n_axes], the pairs of each axis, n_pairs in all.  dealt = 0: the axes
+ * take consecutive runs of pairs; 1: they are dealt pairs in turn (pair i to axis i mod n_axes), an axis that has had its
+ * share leaving its turn to axis 0.  Host only. */
+wnw_status_t wnw_rotary_init(wnw_rotary_t *rotary, int32_t n_pairs, double base, const int32_t *sections, int32_t n_axes,
+                             int32_t dealt, int32_t neighbours);
+
+/* Turns queries and keys by their tokens' positions: with t = positions[axis of the pair][token] * frequency,
+ *   (a, b) -> (a cos t - b sin t, b cos t + a sin t),     inverse = 1: by -t, which is the gradient of the turn by t.
+ *   positions_dev : DEVICE int32 [n_axes] rows of n_tokens, axis_stride elements apart; any value.  The angle is reduced in 64
+ *                   bits, so far positions are as exact as near ones
+ *   q, q_out      : n_tokens rows of heads of head_dim (2 to 256, even) elements of `dtype` (fp32 too); q_out may be q itself,
+ *                   and must not overlap it otherwise
+ *   k, k_out      : the same for the keys, or both NULL
+ * One rounding, at the end.  Strides and alignment are free here (16 bytes are faster). */
+wnw_status_t wnw_rotate(const wnw_rotary_t *rotary, const int32_t *positions_dev, int64_t axis_stride, int32_t n_tokens,
+                        int32_t head_dim, int32_t dtype, const wnw_rows_t *q, const wnw_rows_t *q_out, const wnw_rows_t *k,
+                        const wnw_rows_t *k_out, int32_t inverse, int32_t device, void *cuda_stream);
+
+/* The store.  A block = the rows of one page, one KV head, K or V; it has one scale 2^e, and a stored value is code * 2^e (an
+ * exact bf16 number).
+ *   E4M3  (4 exponent bits, bias 7, 3 mantissa bits, subnormals, largest 448): e the integer with max|x| / 2^e in (224, 448],
+ *         the format of WNW_TIDAL_KV_FP8_E4M3; -110 <= e <= 119
+ *   INT8  -127..127: max|x| / 2^e in (63.5, 127]; -110 <= e <= 121
+ * over the rows a write brings; rows of zeros only have e = -110, so that they never decide a later row's scale.  Codes are
+ * x / 2^e to the nearest, ties to even, infinities and what exceeds the largest code at that code.  Not-a-numbers and infinities
+ * do not count in max|x|; a not-a-number is stored as one in E4M3, as 0 in INT8. */
+enum { WNW_PAGES_E4M3 = 0, WNW_PAGES_INT8 = 1 };
+enum { WNW_PAGES_BAD_PAGE = 1,     /* a page id outside [0, n_pages): its rows were not written; read as zeros; not attended to */
+       WNW_PAGES_BAD_LENGTH = 2 }; /* a length or row range outside the table or the tensors: clipped to what is inside */
+typedef struct {
+  void *codes_dev;          /* DEVICE bytes [n_pages][n_kv_heads][2][page_tokens][head_dim]: K rows, then V rows; 16-byte aligned */
+  float *scales_dev;        /* DEVICE [n_pages][n_kv_heads][2] */
+  int64_t page_stride;      /* bytes from page to page, a multiple of 16; 0: pages are contiguous */
+  int64_t scale_stride;     /* floats from page to page in scales_dev; 0: contiguous */
+  int32_t n_pages;
+  int32_t page_tokens;      /* a multiple of 16, 16..256 */
+  int32_t n_kv_heads;       /* 1..1024 */
+  int32_t head_dim;         /* 64 or 128 */
+  int32_t format;           /* WNW_PAGES_E4M3 or _INT8 */
+  int32_t device;           /* CUDA ordinal of every pointer of a call */
+  int32_t *status_dev;      /* DEVICE word that bits WNW_PAGES_* are OR-ed into, or NULL */
+} wnw_pages_t;
+
+/* A ragged batch: sequence s has rows [row_starts[s], row_starts[s+1]) of the row tensors, and its token t lies in page
+ * page_table[s * table_stride + t / page_tokens], row t mod page_tokens.  lengths, row_starts and page_table are DEVICE int32
+ * and may change between replays of a captured call.  Rows behind the last sequence's are neither read nor written. */
+typedef struct {
+  const int32_t *page_table_dev;  /* [n_seqs][table_stride] */
+  const int32_t *lengths_dev;     /* [n_seqs] */
+  const int32_t *row_starts_dev;  /* [n_seqs + 1], ascending */
+  int32_t table_stride;
+  int32_t n_seqs;                 /* 0..1024 */
+  int32_t n_rows;                 /* rows of the row tensors */
+  int32_t max_rows;               /* the most rows of a sequence, 0: not known.  Shapes the launch only: any value is safe */
+} wnw_batch_t;
+
+/* Quantises new K,V rows into the pages: row i of sequence s becomes its token lengths[s] + i.  A page whose first row is
+ * written starts afresh.  Elsewhere the block's scale is kept, or raised to the one that the new rows need, and then the codes
+ * held before lengths[s] are rounded again for it: code * 2^(e_old - e_new) to the nearest, ties to even.
+ *   k, v          : bf16 or fp16 rows of n_kv_heads heads
+ *   rotary, positions_dev : NULL, or turn the keys on the way (axes as in wnw_rotate, one position per row): the codes are those
+ *                   of wnw_rotate's output.  2 * n_pairs <= head_dim, n_pairs a multiple of 8 (WNW_ERR_UNSUPPORTED)
+ * A page that two sequences of a call write to holds a mixture afterwards; sequences share pages they only read. */
+wnw_status_t wnw_pages_write(const wnw_pages_t *pages, const wnw_batch_t *batch, const wnw_rows_t *k, const wnw_rows_t *v,
+                             int32_t dtype, const wnw_rotary_t *rotary, const int32_t *positions_dev, int64_t axis_stride,
+                             void *cuda_stream);
+
+/* Reads tokens [lengths[s], lengths[s] + rows of s) of every sequence back into k and v (bf16 or fp16; a stored value beyond
+ * fp16's largest becomes that). */
+wnw_status_t wnw_pages_read(const wnw_pages_t *pages, const wnw_batch_t *batch, const wnw_rows_t *k, const wnw_rows_t *v,
+                            int32_t dtype, void *cuda_stream);
+
+/* Attention over the pages: out = softmax(q K^T * softmax_scale) V per query head, over tokens [0, lengths[s]) of the
+ * sequence.  lengths counts the rows' own tokens: row i of n stands at token lengths[s] - n + i, and with causal = 1 sees the
+ * tokens up to that one; with 0 all.  A row that sees nothing (an empty sequence, a row before the first token) gives zeros and a
+ * log-sum-exp of minus infinity.  What a row does not see does not reach it, not-a-numbers included.
+ *   q, out        : bf16 or fp16 rows of n_q_heads heads (a multiple of n_kv_heads, group <= 16; head h reads KV head h / group)
+ *   lse_dev       : NULL or DEVICE float [n_rows][n_q_heads], the log of the sum of exp of the scaled scores
+ *   softmax_scale : 0 -> 1/sqrt(head_dim)
+ *   workspace_dev : wnw_pages_attend_workspace bytes, 256-byte aligned; need not be initialised.  Calls that may overlap in time
+ *                   (two streams, two graphs) need one each */
+wnw_status_t wnw_pages_attend(const wnw_pages_t *pages, const wnw_batch_t *batch, const wnw_rows_t *q, const wnw_rows_t *out,
+                              float *lse_dev, int32_t dtype, int32_t causal, float softmax_scale, void *workspace_dev,
+                              int64_t workspace_bytes, void *cuda_stream);
+wnw_status_t wnw_pages_attend_workspace(const wnw_pages_t *pages, int32_t n_q_heads, int64_t *bytes_host);
+
 const char *wnw_status_string(wnw_status_t status);
 
 #ifdef __cplusplus

@@ -24,6 +24,9 @@ WNW_SCOPE_PER_LAYER, WNW_SCOPE_GLOBAL = 0, 1
 WNW_LAYERS_INDEPENDENT, WNW_LAYERS_CHAINED, WNW_LAYERS_SERIAL, WNW_LAYERS_BATCHED = 0, 1, 2, 3
 WNW_RESIDENCY_HARD_BUDGET, WNW_RESIDENCY_SEGMENT_LAG, WNW_RESIDENCY_SEGMENT_LAG_TOKEN_BASE = 0, 1, 2
 WNW_TIDAL_KV_BF16, WNW_TIDAL_KV_FP8_E4M3 = 0, 1
+WNW_DTYPE_BF16, WNW_DTYPE_FP16, WNW_DTYPE_FP32 = 0, 1, 2
+WNW_PAGES_E4M3, WNW_PAGES_INT8 = 0, 1
+WNW_PAGES_BAD_PAGE, WNW_PAGES_BAD_LENGTH = 1, 2
 
 
 class wnw_config_t(C.Structure):
@@ -38,6 +41,26 @@ class wnw_config_t(C.Structure):
 class wnw_stats_t(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("steps", "hits", "misses", "evictions", "recall_bytes", "resident_audio_tokens",
                                          "host_audio_tokens", "full_audio_tokens")]
+
+
+class wnw_rows_t(C.Structure):
+    _fields_ = [("dev", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("n_heads", C.c_int32), ("reserved", C.c_int32)]
+
+
+class wnw_rotary_t(C.Structure):
+    _fields_ = [("n_pairs", C.c_int32), ("n_axes", C.c_int32), ("neighbours", C.c_int32), ("reserved", C.c_int32),
+                ("frequency", C.c_double * 128), ("axis", C.c_uint8 * 128)]
+
+
+class wnw_pages_t(C.Structure):
+    _fields_ = [("codes_dev", C.c_void_p), ("scales_dev", C.c_void_p), ("page_stride", C.c_int64), ("scale_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("page_tokens", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("format", C.c_int32), ("device", C.c_int32), ("status_dev", C.c_void_p)]
+
+
+class wnw_batch_t(C.Structure):
+    _fields_ = [("page_table_dev", C.c_void_p), ("lengths_dev", C.c_void_p), ("row_starts_dev", C.c_void_p),
+                ("table_stride", C.c_int32), ("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("max_rows", C.c_int32)]
 
 
 class WnwError(RuntimeError):
@@ -91,6 +114,12 @@ _SIGNATURES = {
     "wnw_debug_attend_static_cluster": [_i32, _i32, _i32, _i32, _i32, C.POINTER(_i32)],
     "wnw_attend_static": [_vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32, C.c_float, _i32, _vp],
     "wnw_attend_static_status": [_i32, _vp, C.POINTER(_i32)],
+    "wnw_rotary_init": [C.POINTER(wnw_rotary_t), _i32, C.c_double, C.POINTER(_i32), _i32, _i32, _i32],
+    "wnw_rotate": [_vp, _vp, C.c_int64, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _i32, _i32, _vp],
+    "wnw_pages_write": [_vp, _vp, _vp, _vp, _i32, _vp, _vp, C.c_int64, _vp],
+    "wnw_pages_read": [_vp, _vp, _vp, _vp, _i32, _vp],
+    "wnw_pages_attend": [_vp, _vp, _vp, _vp, _vp, _i32, _i32, C.c_float, _vp, C.c_int64, _vp],
+    "wnw_pages_attend_workspace": [_vp, _i32, C.POINTER(C.c_int64)],
 }
 
 
@@ -429,3 +458,170 @@ def wnw_debug_attend_static_cluster(n_tokens: int, n_q_heads: int, n_kv_heads: i
     v = _i32()
     _ck(lib().wnw_debug_attend_static_cluster(device, n_tokens, n_q_heads, n_kv_heads, head_dim, C.byref(v)), "wnw_debug_attend_static_cluster")
     return v.value
+
+
+# ---- operators around a caller-owned, paged K/V store of eight bits ----
+_dtypes = None    # torch's element types by the library's
+
+
+def _dtype(t) -> int:
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {torch.bfloat16: WNW_DTYPE_BF16, torch.float16: WNW_DTYPE_FP16, torch.float32: WNW_DTYPE_FP32}
+    return _dtypes.get(t.dtype, -1)
+
+
+def _stream_on(stream, device: int) -> Optional[int]:
+    """The given stream, else the current one of the device that the call's tensors are on."""
+    if stream is not None:
+        return int(stream.cuda_stream) or None
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device) or None
+
+
+def _refuse(what: str, why: str):
+    raise WnwError(WNW_ERR_INVALID_ARG, f"{what} ({why})")
+
+
+def _rows(t, what: str, dtype=None, device=None, head_dim=None):
+    """A tensor [rows, heads, head_dim] as the library takes it."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or (stride[2] != 1 and shape[2] != 1):
+        _refuse(what, "rows of heads: [rows, heads, head_dim], innermost contiguous")
+    if dtype is not None and t.dtype != dtype:
+        _refuse(what, "tensors of one type")
+    if t.get_device() < 0 or (device is not None and t.get_device() != device):
+        _refuse(what, "tensors on one CUDA device")
+    if head_dim is not None and shape[2] != head_dim:
+        _refuse(what, "head_dim")
+    return wnw_rows_t(t.data_ptr(), stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else 0, shape[1], 0)
+
+
+def _ints(t, what: str, name: str, device: int, dims: int):
+    import torch
+    if t.dtype != torch.int32 or t.dim() != dims or t.get_device() != device or (t.numel() and t.stride(-1) != 1):
+        _refuse(what, f"{name}: int32, {dims}-dimensional, innermost contiguous, on the device of the others")
+    return t
+
+
+def wnw_rotary_init(n_pairs: int, base: float, sections: Optional[Sequence[int]] = None, dealt: bool = False,
+                    neighbours: bool = False) -> wnw_rotary_t:
+    """The plan of a rotary encoding.  sections: pairs of each axis (default: one axis)."""
+    sections = [n_pairs] if sections is None else list(sections)
+    r = wnw_rotary_t()
+    _ck(lib().wnw_rotary_init(C.byref(r), n_pairs, base, (_i32 * len(sections))(*sections), len(sections), int(dealt), int(neighbours)),
+        "wnw_rotary_init")
+    return r
+
+
+def _positions(positions, rotary, n_rows: int, device: int, what: str):
+    """[axes, rows], or [rows] for one axis; returns (pointer, elements between the axes)."""
+    if positions.dim() == 1:
+        positions = positions.unsqueeze(0)
+    _ints(positions, what, "positions", device, 2)
+    if tuple(positions.shape) != (rotary.n_axes, n_rows):
+        _refuse(what, "positions: one per axis and row")
+    return positions.data_ptr(), positions.stride(0)
+
+
+def wnw_rotate(rotary, positions, q, q_out, k=None, k_out=None, inverse=False, stream=None):
+    """q, k: [n_tokens, heads, head_dim] bf16, fp16 or fp32 CUDA tensors, any strides with the innermost contiguous; q_out and
+    k_out may be q and k.  positions: int32 [n_axes, n_tokens].  inverse: the gradient of the turn."""
+    device, n, head_dim = q.get_device(), q.shape[0], q.shape[-1]
+    rows = [_rows(q, "wnw_rotate"), _rows(q_out, "wnw_rotate", q.dtype, device, head_dim)]
+    if q_out.shape != q.shape or (k is None) != (k_out is None):
+        _refuse("wnw_rotate", "an output of the shape of its input")
+    if k is not None:
+        if k.shape[0] != n or k_out.shape != k.shape:
+            _refuse("wnw_rotate", "as many keys as queries, an output of the shape of its input")
+        rows += [_rows(k, "wnw_rotate", q.dtype, device, head_dim), _rows(k_out, "wnw_rotate", q.dtype, device, head_dim)]
+    at, axis_stride = _positions(positions, rotary, n, device, "wnw_rotate")
+    refs = [C.byref(x) for x in rows] + [None] * (4 - len(rows))
+    _ck(lib().wnw_rotate(C.byref(rotary), at, axis_stride, n, head_dim, _dtype(q), *refs, int(inverse), device, _stream_on(stream, device)),
+        "wnw_rotate")
+
+
+def wnw_pages(codes, scales, status=None) -> wnw_pages_t:
+    """The handle of a store: codes [n_pages, n_kv_heads, 2, page_tokens, head_dim], float8_e4m3fn (or uint8, taken as that) or int8;
+    scales float32 [n_pages, n_kv_heads, 2]; status: an int32 CUDA tensor that WNW_PAGES_* bits are OR-ed into.  Pages may lie
+    apart; what is inside a page is contiguous.  The tensors must outlive the handle."""
+    import torch
+    formats = {torch.float8_e4m3fn: WNW_PAGES_E4M3, torch.uint8: WNW_PAGES_E4M3, torch.int8: WNW_PAGES_INT8}
+    if codes.dtype not in formats or codes.dim() != 5 or codes.shape[2] != 2:
+        _refuse("wnw_pages", "codes: [n_pages, n_kv_heads, 2, page_tokens, head_dim] of one byte each")
+    n, h, _, t, d = codes.shape
+    device = codes.get_device()
+    if scales.dtype != torch.float32 or tuple(scales.shape) != (n, h, 2) or scales.get_device() != device or device < 0:
+        _refuse("wnw_pages", "scales: float32 [n_pages, n_kv_heads, 2] on the codes' CUDA device")
+    if n and (not codes[0].is_contiguous() or not scales[0].is_contiguous()):
+        _refuse("wnw_pages", "a page is contiguous")
+    if status is not None and (status.dtype != torch.int32 or status.numel() < 1 or status.get_device() != device):
+        _refuse("wnw_pages", "status: an int32 tensor on the codes' CUDA device")
+    return wnw_pages_t(codes.data_ptr(), scales.data_ptr(), codes.stride(0) if n > 1 else 0, scales.stride(0) if n > 1 else 0, n, t, h, d,
+                       formats[codes.dtype], device, _ptr(status))
+
+
+def _batch(pages, page_table, lengths, row_starts, n_rows: int, max_rows: int, what: str):
+    device, n = pages.device, lengths.shape[0]
+    _ints(page_table, what, "page_table", device, 2)
+    _ints(lengths, what, "lengths", device, 1)
+    _ints(row_starts, what, "row_starts", device, 1)
+    if page_table.shape[0] != n or row_starts.shape[0] != n + 1:
+        _refuse(what, "page_table, lengths and row_starts of one batch")
+    stride = page_table.stride(0) if n > 1 else page_table.shape[1]
+    if stride < page_table.shape[1]:
+        _refuse(what, "page_table: sequences apart from one another")
+    return wnw_batch_t(page_table.data_ptr(), lengths.data_ptr(), row_starts.data_ptr(), stride, n, n_rows, max_rows)
+
+
+def _kv_rows(pages, k, v, what: str):
+    if k.shape != v.shape:
+        _refuse(what, "k and v of one shape")
+    return _rows(k, what, None, pages.device, pages.head_dim), _rows(v, what, k.dtype, pages.device, pages.head_dim)
+
+
+def wnw_pages_write(pages, page_table, lengths, row_starts, k, v, rotary=None, positions=None, max_rows=0, stream=None):
+    """k, v: [n_rows, n_kv_heads, head_dim] bf16 or fp16; row i of sequence s becomes its token lengths[s] + i.  With rotary and
+    positions (int32 [n_axes, n_rows]) the keys are turned on the way."""
+    rk, rv = _kv_rows(pages, k, v, "wnw_pages_write")
+    batch = _batch(pages, page_table, lengths, row_starts, k.shape[0], max_rows, "wnw_pages_write")
+    at, axis_stride = None, 0
+    if (rotary is None) != (positions is None):
+        _refuse("wnw_pages_write", "rotary and positions go together")
+    if rotary is not None:
+        at, axis_stride = _positions(positions, rotary, k.shape[0], pages.device, "wnw_pages_write")
+    _ck(lib().wnw_pages_write(C.byref(pages), C.byref(batch), C.byref(rk), C.byref(rv), _dtype(k), None if rotary is None else C.byref(rotary),
+                              at, axis_stride, _stream_on(stream, pages.device)), "wnw_pages_write")
+
+
+def wnw_pages_read(pages, page_table, lengths, row_starts, k, v, max_rows=0, stream=None):
+    """Tokens lengths[s], lengths[s] + 1, ... of every sequence into its rows of k and v [n_rows, n_kv_heads, head_dim]."""
+    rk, rv = _kv_rows(pages, k, v, "wnw_pages_read")
+    batch = _batch(pages, page_table, lengths, row_starts, k.shape[0], max_rows, "wnw_pages_read")
+    _ck(lib().wnw_pages_read(C.byref(pages), C.byref(batch), C.byref(rk), C.byref(rv), _dtype(k), _stream_on(stream, pages.device)),
+        "wnw_pages_read")
+
+
+def wnw_pages_attend_workspace(pages, n_q_heads: int) -> int:
+    """Bytes of workspace that wnw_pages_attend needs, whatever the batch."""
+    n = C.c_int64()
+    _ck(lib().wnw_pages_attend_workspace(C.byref(pages), n_q_heads, C.byref(n)), "wnw_pages_attend_workspace")
+    return n.value
+
+
+def wnw_pages_attend(pages, page_table, lengths, row_starts, q, out, workspace, lse=None, causal=True, softmax_scale=0.0, max_rows=0,
+                     stream=None):
+    """q, out: [n_rows, n_q_heads, head_dim] bf16 or fp16; lse: None or float32 [n_rows, n_q_heads]; workspace: a CUDA tensor of
+    wnw_pages_attend_workspace bytes."""
+    device, what = pages.device, "wnw_pages_attend"
+    rq, ro = _rows(q, what, None, device, pages.head_dim), _rows(out, what, q.dtype, device, pages.head_dim)
+    if q.shape != out.shape:
+        _refuse(what, "an output of the queries' shape")
+    batch = _batch(pages, page_table, lengths, row_starts, q.shape[0], max_rows, what)
+    if lse is not None and (str(lse.dtype) != "torch.float32" or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.get_device() != device):
+        _refuse(what, "lse: float32 [n_rows, n_q_heads], contiguous")
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        _refuse(what, "workspace: contiguous, on the pages' device")
+    _ck(lib().wnw_pages_attend(C.byref(pages), C.byref(batch), C.byref(rq), C.byref(ro), _ptr(lse), _dtype(q), int(causal), softmax_scale,
+                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_on(stream, device)), what)

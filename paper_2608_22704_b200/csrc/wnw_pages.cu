@@ -1,0 +1,373 @@
+// The paged K/V store of eight bits: quantising rows as they are written (wnw_pages_write) and reading them back (wnw_pages_read).
+//
+// Power-of-two scales make all of it exact but the one rounding to the code: x / 2^e is x with another exponent, code * 2^e a bf16
+// number, and a scale that is raised rounds integers (or subnormal e4m3 numbers) again.  Both directions move each element once, so
+// memory bounds them; a CTA takes one page of one KV head, K or V, whose scale it thereby owns: no atomics, one order of everything.
+#include <algorithm>
+#include <atomic>
+
+#include "wnw_pages.cuh"
+
+namespace wnw {
+namespace {
+
+// ---- codes ----
+template <int FMT> __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
+  if constexpr (FMT == WNW_PAGES_E4M3) {
+    unsigned short lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;\n" : "=h"(lo) : "f"(a), "f"(b));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;\n" : "=h"(hi) : "f"(c), "f"(d));
+    return lo | (uint32_t)hi << 16;
+  } else {
+    const int i = max(-127, min(127, __float2int_rn(a))), j = max(-127, min(127, __float2int_rn(b)));   // not-a-number: 0
+    const int k = max(-127, min(127, __float2int_rn(c))), l = max(-127, min(127, __float2int_rn(d)));
+    return (i & 255) | (j & 255) << 8 | (k & 255) << 16 | (uint32_t)l << 24;
+  }
+}
+template <int FMT> __device__ __forceinline__ void decode4(uint32_t w, float (&x)[4]) {
+  if constexpr (FMT == WNW_PAGES_E4M3) {
+    uint32_t lo, hi;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(lo) : "h"((unsigned short)w));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(hi) : "h"((unsigned short)(w >> 16)));
+    const float2 f = Pair<__half>::get(lo), g = Pair<__half>::get(hi);
+    x[0] = f.x; x[1] = f.y; x[2] = g.x; x[3] = g.y;
+  } else {
+    x[0] = (float)(int)(signed char)w; x[1] = (float)(int)(signed char)(w >> 8);
+    x[2] = (float)(int)(signed char)(w >> 16); x[3] = (float)((int)w >> 24);
+  }
+}
+// the scale's exponent for rows whose largest magnitude has these bits
+template <int FMT> __device__ __forceinline__ int exponent_for(uint32_t bits) {
+  // 448 = 1.75 * 2^8; 127 = 1.984375 * 2^6
+  const int e = (int)(bits >> 23) - 127 - (FMT == WNW_PAGES_E4M3 ? 8 : 6) + ((bits & 0x7fffff) > (FMT == WNW_PAGES_E4M3 ? 0x600000u : 0x7e0000u));
+  return max(PG_LOWEST, min(pg_highest(FMT), e));
+}
+__device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// What of a sequence a call covers: tokens [first, end), rows from row0 on; everything inside the table and the tensors
+struct Span { int first, end, row0; };
+__device__ __forceinline__ Span span_of(const PagesView &pv, const BatchView &b, int s) {
+  int r0 = b.starts[s], r1 = b.starts[s + 1], n = b.lengths[s];
+  const int cap = b.stride * pv.T;      // (checked on the host to fit)
+  if (r0 < 0 || r1 < r0 || r1 > b.n_rows || n < 0 || n > cap || r1 - r0 > cap - n) {
+    if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) pg_report(pv, WNW_PAGES_BAD_LENGTH);
+    if (r0 < 0 || r1 < r0 || n < 0) return Span{0, 0, 0};
+    r1 = min(r1, b.n_rows);
+    r0 = min(r0, r1);
+    n = min(n, cap);
+  }
+  return Span{n, n + min(r1 - r0, cap - n), r0};
+}
+
+// ---- write ----
+struct WriteArgs {
+  PagesView pv;
+  BatchView bv;
+  RowsView in[2];                    // K, V
+  RotaryView rot;                    // n_pairs = 0: keys are written as they are
+  const int32_t *positions;
+  long long axis_stride;
+};
+
+// Elements that a thread takes at a time: 8 from `lo` on and 8 from `hi` on, so that the turn of a pair stays in the thread.
+template <int D> __device__ __forceinline__ void unit_offsets(int u, int n_pairs, int neighbours, int *lo, int *hi) {
+  const int turned = n_pairs / 8;
+  if (u < turned && !neighbours) { *lo = 8 * u; *hi = 8 * u + n_pairs; }
+  else { *lo = 16 * u; *hi = 16 * u + 8; }             // also what lies behind the pairs: 2 * n_pairs + 16 * (u - turned)
+}
+
+// CTA: (pages of a sequence, one at a time; KV head and K|V; sequence).  UN units of 16 elements a thread at most.
+template <typename T, int D, int FMT, int UN, int THREADS>
+__global__ void __launch_bounds__(THREADS) wnw_pages_write_kernel(const __grid_constant__ WriteArgs a) {
+  constexpr int UPR = D / 16;                          // units of a row
+  __shared__ uint32_t red[16];
+  const PagesView &pv = a.pv;
+  const int s = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1, nt = THREADS;
+  const Span sp = span_of(pv, a.bv, s);
+  if (sp.first >= sp.end) return;
+  const bool turn = a.rot.n_pairs && which == 0;
+  const int page0 = sp.first / pv.T, n_touched = (sp.end - 1) / pv.T - page0 + 1;
+  for (int i = blockIdx.x; i < n_touched; i += gridDim.x) {
+    const int base = (page0 + i) * pv.T, t0 = max(sp.first, base) - base, t1 = min(sp.end - base, pv.T);
+    const int page = a.bv.table[(long long)s * a.bv.stride + page0 + i];
+    if (page < 0 || page >= pv.n_pages) {
+      if (threadIdx.x == 0) pg_report(pv, WNW_PAGES_BAD_PAGE);
+      continue;
+    }
+    float *scale = pv.scales + page * pv.scale_stride + head * 2 + which;
+    const float old_scale = t0 ? *scale : 0.f;         // needed late, asked for early
+    uint4 x[UN][2];
+    uint32_t most = 0;
+    const int n_units = (t1 - t0) * UPR;
+#pragma unroll
+    for (int j = 0; j < UN; ++j) {
+      const int u = threadIdx.x + j * nt;
+      x[j][0] = x[j][1] = make_uint4(0, 0, 0, 0);
+      if (u < n_units) {
+        const int r = u / UPR;
+        int lo, hi;
+        unit_offsets<D>(u % UPR, turn ? a.rot.n_pairs : 0, a.rot.neighbours, &lo, &hi);
+        const T *p = reinterpret_cast<const T *>(a.in[which].p) + (long long)(sp.row0 + base + t0 + r - sp.first) * a.in[which].row + head * a.in[which].head;
+        x[j][0] = *reinterpret_cast<const uint4 *>(p + lo);
+        x[j][1] = *reinterpret_cast<const uint4 *>(p + hi);
+      }
+    }
+    if (turn) {
+#pragma unroll
+      for (int j = 0; j < UN; ++j) {
+        const int u = threadIdx.x + j * nt, p0 = 8 * (u % UPR);
+        if (u < n_units && p0 < a.rot.n_pairs) {
+          const int row = sp.row0 + base + t0 + u / UPR - sp.first;
+          uint32_t w[8] = {x[j][0].x, x[j][0].y, x[j][0].z, x[j][0].w, x[j][1].x, x[j][1].y, x[j][1].z, x[j][1].w};
+          if (a.rot.neighbours) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const float2 c = pg_angle(a.rot, p0 + q, a.positions[a.rot.axis[p0 + q] * a.axis_stride + row]);
+              const float2 f = Pair<T>::get(w[q]);
+              const float2 t = pg_turn(f.x, f.y, c);
+              w[q] = Pair<T>::put(t.x, t.y);
+            }
+          } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const float2 c = pg_angle(a.rot, p0 + 2 * q, a.positions[a.rot.axis[p0 + 2 * q] * a.axis_stride + row]);
+              const float2 d = pg_angle(a.rot, p0 + 2 * q + 1, a.positions[a.rot.axis[p0 + 2 * q + 1] * a.axis_stride + row]);
+              const float2 f = Pair<T>::get(w[q]), g = Pair<T>::get(w[4 + q]);
+              const float2 t = pg_turn(f.x, g.x, c), z = pg_turn(f.y, g.y, d);
+              w[q] = Pair<T>::put(t.x, z.x);
+              w[4 + q] = Pair<T>::put(t.y, z.y);
+            }
+          }
+          x[j][0] = make_uint4(w[0], w[1], w[2], w[3]);
+          x[j][1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < UN; ++j) {
+      const uint32_t w[8] = {x[j][0].x, x[j][0].y, x[j][0].z, x[j][0].w, x[j][1].x, x[j][1].y, x[j][1].z, x[j][1].w};
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float2 f = Pair<T>::get(w[q]);
+        const uint32_t m = __float_as_uint(f.x) & 0x7fffffffu, n = __float_as_uint(f.y) & 0x7fffffffu;
+        most = max(most, m < 0x7f800000u ? m : 0u);
+        most = max(most, n < 0x7f800000u ? n : 0u);
+      }
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = most;
+    __syncthreads();
+    for (int w = 0; w < nt / 32; ++w) most = max(most, red[w]);
+    __syncthreads();                                   // red is free for the next page
+    int e = exponent_for<FMT>(most);
+    unsigned char *block = pv.codes + page * pv.page_stride + (long long)(head * 2 + which) * pv.T * D;
+    if (t0) {
+      const int had = max(PG_LOWEST, min(pg_highest(FMT), (int)(__float_as_uint(old_scale) >> 23 & 255) - 127));
+      if (e > had) {                                   // rows of before, for the raised scale
+        const float down = power(max(-64, had - e));   // (codes / 2^64 are 0 already)
+        for (int u = threadIdx.x; u < t0 * (D / 16); u += nt) {
+          uint4 *p = reinterpret_cast<uint4 *>(block + (long long)u * 16), v = *p;
+          uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float f[4];
+            decode4<FMT>(w[q], f);
+            w[q] = encode4<FMT>(f[0] * down, f[1] * down, f[2] * down, f[3] * down);
+          }
+          *p = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+      e = max(e, had);
+    }
+    if (threadIdx.x == 0) *scale = power(e);
+    const float by = power(-e);
+#pragma unroll
+    for (int j = 0; j < UN; ++j) {
+      const int u = threadIdx.x + j * nt;
+      if (u < n_units) {
+        int lo, hi;
+        unit_offsets<D>(u % UPR, turn ? a.rot.n_pairs : 0, a.rot.neighbours, &lo, &hi);
+        unsigned char *p = block + (long long)(t0 + u / UPR) * D;
+        const uint32_t w[8] = {x[j][0].x, x[j][0].y, x[j][0].z, x[j][0].w, x[j][1].x, x[j][1].y, x[j][1].z, x[j][1].w};
+        uint32_t c[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float2 f = Pair<T>::get(w[2 * q]), g = Pair<T>::get(w[2 * q + 1]);
+          c[q] = encode4<FMT>(f.x * by, f.y * by, g.x * by, g.y * by);
+        }
+        *reinterpret_cast<uint2 *>(p + lo) = make_uint2(c[0], c[1]);
+        *reinterpret_cast<uint2 *>(p + hi) = make_uint2(c[2], c[3]);
+      }
+    }
+  }
+}
+
+// ---- read ----
+struct ReadArgs {
+  PagesView pv;
+  BatchView bv;
+  RowsView out[2];
+};
+
+template <typename T, int D, int FMT>
+__global__ void __launch_bounds__(256) wnw_pages_read_kernel(const __grid_constant__ ReadArgs a) {
+  constexpr int UPR = D / 16;
+  const PagesView &pv = a.pv;
+  const int s = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1, nt = blockDim.x;
+  const Span sp = span_of(pv, a.bv, s);
+  if (sp.first >= sp.end) return;
+  const int page0 = sp.first / pv.T, n_touched = (sp.end - 1) / pv.T - page0 + 1;
+  for (int i = blockIdx.x; i < n_touched; i += gridDim.x) {
+    const int base = (page0 + i) * pv.T, t0 = max(sp.first, base) - base, t1 = min(sp.end - base, pv.T);
+    const int page = a.bv.table[(long long)s * a.bv.stride + page0 + i];
+    const bool there = page >= 0 && page < pv.n_pages;
+    if (!there && threadIdx.x == 0) pg_report(pv, WNW_PAGES_BAD_PAGE);
+    const float scale = there ? pv.scales[page * pv.scale_stride + head * 2 + which] : 0.f;
+    const unsigned char *block = pv.codes + (there ? page : 0) * pv.page_stride + (long long)(head * 2 + which) * pv.T * D;
+    for (int u = threadIdx.x; u < (t1 - t0) * UPR; u += nt) {
+      const int r = u / UPR, c = u % UPR;
+      const uint4 v = there ? *reinterpret_cast<const uint4 *>(block + (long long)(t0 + r) * D + 16 * c) : make_uint4(0, 0, 0, 0);
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      uint32_t o[8];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float f[4];
+        decode4<FMT>(w[q], f);
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          f[z] *= scale;
+          if (sizeof(T) == 2 && std::is_same<T, __half>::value && fabsf(f[z]) > 65504.f) f[z] = copysignf(65504.f, f[z]);
+        }
+        o[2 * q] = Pair<T>::put(f[0], f[1]);
+        o[2 * q + 1] = Pair<T>::put(f[2], f[3]);
+      }
+      T *p = reinterpret_cast<T *>(a.out[which].p) + (long long)(sp.row0 + base + t0 + r - sp.first) * a.out[which].row + head * a.out[which].head + 16 * c;
+      reinterpret_cast<uint4 *>(p)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+      reinterpret_cast<uint4 *>(p)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+    }
+  }
+}
+
+// Pages that a sequence's rows can touch, by what the caller says of the rows; the kernels' loops cover the rest.
+int pages_touched(const wnw_batch_t &b, int T) {
+  const int rows = b.max_rows > 0 ? std::min(b.max_rows, b.n_rows) : b.n_rows;
+  return std::min((rows + T - 2) / T + 1, 65536);
+}
+
+template <typename T, int D, int FMT> cudaError_t launch_write(const WriteArgs &a, dim3 grid, cudaStream_t st) {
+  const int units = a.pv.T * (D / 16);
+  if (units <= 512) wnw_pages_write_kernel<T, D, FMT, 2, 256><<<grid, 256, 0, st>>>(a);
+  else if (units <= 1024) wnw_pages_write_kernel<T, D, FMT, 4, 256><<<grid, 256, 0, st>>>(a);
+  else wnw_pages_write_kernel<T, D, FMT, 4, 512><<<grid, 512, 0, st>>>(a);
+  return cudaGetLastError();
+}
+template <typename T> cudaError_t launch_write(const WriteArgs &a, int d, int fmt, dim3 grid, cudaStream_t st) {
+  if (d == 64) return fmt == WNW_PAGES_E4M3 ? launch_write<T, 64, WNW_PAGES_E4M3>(a, grid, st) : launch_write<T, 64, WNW_PAGES_INT8>(a, grid, st);
+  return fmt == WNW_PAGES_E4M3 ? launch_write<T, 128, WNW_PAGES_E4M3>(a, grid, st) : launch_write<T, 128, WNW_PAGES_INT8>(a, grid, st);
+}
+template <typename T> cudaError_t launch_read(const ReadArgs &a, int d, int fmt, dim3 grid, cudaStream_t st) {
+  if (d == 64) {
+    if (fmt == WNW_PAGES_E4M3) wnw_pages_read_kernel<T, 64, WNW_PAGES_E4M3><<<grid, 256, 0, st>>>(a);
+    else wnw_pages_read_kernel<T, 64, WNW_PAGES_INT8><<<grid, 256, 0, st>>>(a);
+  } else {
+    if (fmt == WNW_PAGES_E4M3) wnw_pages_read_kernel<T, 128, WNW_PAGES_E4M3><<<grid, 256, 0, st>>>(a);
+    else wnw_pages_read_kernel<T, 128, WNW_PAGES_INT8><<<grid, 256, 0, st>>>(a);
+  }
+  return cudaGetLastError();
+}
+
+wnw_status_t check_kv_rows(const wnw_pages_t *p, const wnw_batch_t *b, const wnw_rows_t *k, const wnw_rows_t *v, int dtype) {
+  if (!k || !v) return WNW_ERR_INVALID_ARG;
+  if (dtype != WNW_DTYPE_BF16 && dtype != WNW_DTYPE_FP16) return WNW_ERR_UNSUPPORTED;
+  for (const wnw_rows_t *r : {k, v})
+    if (r->n_heads != p->n_kv_heads || (b->n_rows && (!r->dev || !pg_vector_rows(*r, dtype)))) return WNW_ERR_INVALID_ARG;
+  return WNW_OK;
+}
+
+}  // namespace
+
+wnw_status_t pg_view(const wnw_pages_t *p, PagesView *v) {
+  if (!p || p->n_pages < 0 || p->page_stride < 0 || p->scale_stride < 0) return WNW_ERR_INVALID_ARG;
+  if (p->head_dim != 64 && p->head_dim != 128) return WNW_ERR_UNSUPPORTED;
+  if (p->page_tokens < PG_GR || p->page_tokens > PG_MAX_PAGE || p->page_tokens % PG_GR) return WNW_ERR_UNSUPPORTED;
+  if (p->n_kv_heads < 1 || p->format < WNW_PAGES_E4M3 || p->format > WNW_PAGES_INT8) return WNW_ERR_INVALID_ARG;
+  if (p->n_kv_heads > 1024) return WNW_ERR_CAPACITY;
+  const long long page = 2ll * p->n_kv_heads * p->page_tokens * p->head_dim, scales = 2ll * p->n_kv_heads;
+  if (p->n_pages && (!p->codes_dev || !p->scales_dev || (uintptr_t)p->codes_dev % 16 || (uintptr_t)p->scales_dev % 4)) return WNW_ERR_INVALID_ARG;
+  if ((p->page_stride && (p->page_stride < page || p->page_stride % 16)) || (p->scale_stride && p->scale_stride < scales)) return WNW_ERR_INVALID_ARG;
+  if ((uintptr_t)p->status_dev % 4) return WNW_ERR_INVALID_ARG;
+  *v = PagesView{(unsigned char *)p->codes_dev, p->scales_dev, p->page_stride ? (long long)p->page_stride : page, p->scale_stride ? (long long)p->scale_stride : scales,
+                 p->n_pages, p->page_tokens, p->n_kv_heads, p->status_dev};
+  return WNW_OK;
+}
+
+wnw_status_t pg_view(const wnw_pages_t *p, const wnw_batch_t *b, PagesView *pv, BatchView *bv) {
+  const wnw_status_t rc = pg_view(p, pv);
+  if (rc != WNW_OK) return rc;
+  if (!b || b->n_seqs < 0 || b->n_rows < 0 || b->max_rows < 0 || b->table_stride < 0) return WNW_ERR_INVALID_ARG;
+  if (b->n_seqs > PG_MAX_SEQS || (long long)b->table_stride * p->page_tokens > 1ll << 30) return WNW_ERR_CAPACITY;
+  if (b->n_seqs && (!b->lengths_dev || !b->row_starts_dev || (b->table_stride && !b->page_table_dev))) return WNW_ERR_INVALID_ARG;
+  for (const void *q : {(const void *)b->page_table_dev, (const void *)b->lengths_dev, (const void *)b->row_starts_dev})
+    if ((uintptr_t)q % 4) return WNW_ERR_INVALID_ARG;
+  *bv = BatchView{b->page_table_dev, b->lengths_dev, b->row_starts_dev, b->table_stride, b->n_seqs, b->n_rows};
+  return WNW_OK;
+}
+
+wnw_status_t pg_sms(int device, int *n) {
+  static std::atomic<int> known[64];
+  if (device < 0 || device >= 64) return WNW_ERR_INVALID_ARG;
+  int v = known[device].load(std::memory_order_relaxed);
+  if (!v) {
+    if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) { cudaGetLastError(); return WNW_ERR_CUDA; }
+    known[device].store(v, std::memory_order_relaxed);
+  }
+  *n = v;
+  return WNW_OK;
+}
+
+}  // namespace wnw
+
+using namespace wnw;
+
+extern "C" wnw_status_t wnw_pages_write(const wnw_pages_t *pages, const wnw_batch_t *batch, const wnw_rows_t *k, const wnw_rows_t *v,
+                                        int32_t dtype, const wnw_rotary_t *rotary, const int32_t *positions_dev, int64_t axis_stride,
+                                        void *cuda_stream) {
+  WriteArgs a;
+  wnw_status_t rc = pg_view(pages, batch, &a.pv, &a.bv);
+  if (rc != WNW_OK || (rc = check_kv_rows(pages, batch, k, v, dtype)) != WNW_OK) return rc;
+  a.rot.n_pairs = 0;
+  if (rotary) {
+    if ((rc = rotary_view(rotary, pages->head_dim, 0, &a.rot)) != WNW_OK) return rc;
+    if (a.rot.n_pairs % 8) return WNW_ERR_UNSUPPORTED;
+    if (batch->n_rows && (!positions_dev || (uintptr_t)positions_dev % 4)) return WNW_ERR_INVALID_ARG;
+  }
+  a.positions = positions_dev;
+  a.axis_stride = axis_stride;
+  a.in[0] = rows_view(*k);
+  a.in[1] = rows_view(*v);
+  if (!batch->n_seqs || !batch->n_rows) return WNW_OK;
+  OnDevice on(pages->device);
+  if (!on.ok) return WNW_ERR_CUDA;
+  const dim3 grid(pages_touched(*batch, pages->page_tokens), 2 * pages->n_kv_heads, batch->n_seqs);
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const cudaError_t e = dtype == WNW_DTYPE_BF16 ? launch_write<__nv_bfloat16>(a, pages->head_dim, pages->format, grid, st)
+                                                : launch_write<__half>(a, pages->head_dim, pages->format, grid, st);
+  return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
+}
+
+extern "C" wnw_status_t wnw_pages_read(const wnw_pages_t *pages, const wnw_batch_t *batch, const wnw_rows_t *k, const wnw_rows_t *v,
+                                       int32_t dtype, void *cuda_stream) {
+  ReadArgs a;
+  wnw_status_t rc = pg_view(pages, batch, &a.pv, &a.bv);
+  if (rc != WNW_OK || (rc = check_kv_rows(pages, batch, k, v, dtype)) != WNW_OK) return rc;
+  a.out[0] = rows_view(*k);
+  a.out[1] = rows_view(*v);
+  if (!batch->n_seqs || !batch->n_rows) return WNW_OK;
+  OnDevice on(pages->device);
+  if (!on.ok) return WNW_ERR_CUDA;
+  const dim3 grid(pages_touched(*batch, pages->page_tokens), 2 * pages->n_kv_heads, batch->n_seqs);
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const cudaError_t e = dtype == WNW_DTYPE_BF16 ? launch_read<__nv_bfloat16>(a, pages->head_dim, pages->format, grid, st)
+                                                : launch_read<__half>(a, pages->head_dim, pages->format, grid, st);
+  return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
+}

@@ -1,0 +1,701 @@
+// wnw_pages_attend: attention of a ragged batch of query rows over the paged eight-bit store.
+//
+//   s = (q . code_k) * 2^eK * scale,   p = softmax of s over the tokens that the row sees,   out = sum p * code_v * 2^eV
+//
+// What bounds it with few query rows: reading the codes, one byte an element.  So the schedule is even in bytes: the granules (16
+// tokens of a KV head) of all sequences lie on one line, every CTA takes an equal stretch of it, found on the device from the lengths,
+// and a head's stretches meet again in wnw_pages_join_kernel.  Within a CTA the granules go round the warps, each with a softmax of its
+// own, which meet in shared memory where a head ends.
+//
+// A warp multiplies tokens x head_dim by head_dim x query rows (S^T = K Q^T, O^T = V^T P^T; mma.sync m16n8k16), so that a group of up
+// to eight query rows fills an operand.  The order of the contracted index is free as long as both operands agree, so every lane keeps
+// to bytes that it copied itself: 16 of a row at a time, asynchronously into a ring of its own in shared memory, with no barrier and no
+// bank conflict.  Codes become fp16 exactly (e4m3 has 4 significant bits, int8 8); the query is scaled by a power of two to the top of
+// fp16's range (exact but for elements 2^-32 of its largest); weights are fp16 against a reference within 2^8 of the largest.  Sums,
+// maxima and accumulators are fp32.
+//
+// The scales 2^eV sit inside the sum over tokens.  A second reference M, the maximum of s + eV in log2, carries them: weights enter the
+// product as 2^(s + eV - M), the denominator as 2^(s - m), and out = product * 2^(M - m) / denominator.  No spread of scales over the
+// pages can push the weights that matter out of fp16's range.
+#include <algorithm>
+#include <atomic>
+#include <cstring>
+
+#include "wnw_pages.cuh"
+
+namespace wnw {
+namespace {
+
+constexpr int PA_WARPS = 8, PA_THREADS = PA_WARPS * 32;
+constexpr int PA_STAGES = 4;         // granules of a warp in the ring
+constexpr int PA_SEGS = 64;          // stretches of heads that a CTA prepares at a time
+constexpr int PA_ROWS = 16;          // query rows of a partial result
+constexpr float LAZY = 8.f;          // log2 by which a score may exceed the reference before that follows
+
+// ---- workspace: per CTA two partial results (a head begun before, a head not finished) ----
+struct PartHead { int item, n_parts; };        // of slot 1: which head, how many CTAs share it; n_parts = 0: none
+struct PartRow { float m, big_m, l, pad; };
+
+struct AttendArgs {
+  PagesView pv;
+  BatchView bv;
+  RowsView q, out;
+  float *lse;
+  int Hq, g, rt;                     // query heads, group, query tokens of a tile
+  int dtype, causal;
+  float scale_log2;
+  float *part_o;                     // [CTA][2][PA_ROWS][D]
+  PartRow *part_row;                 // [CTA][2][PA_ROWS]
+  PartHead *part_head;               // [CTA]
+};
+
+// A head's stretch inside a CTA.
+struct Seg {
+  int s, h, tile;                    // sequence, KV head, tile of query tokens
+  int g0, n, y0;                     // first granule, granules, place of the first on the CTA's line
+  int need;                          // granules from the head's first on that some row sees
+  int len, row0, nq;                 // tokens of the sequence; first query row and query tokens of the tile
+  int end0;                          // tokens that the tile's first query row sees; the next rows see one more each if causal
+  int item, slot, n_parts;           // slot -1: the whole head; else where the partial result goes
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {   // an 8 x 8 matrix of 16-bit elements over the warp
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool there) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;\n" ::"r"(dst), "l"(src), "r"(there ? 8 : 0) : "memory");
+}
+
+// Four codes as fp16: the lower two in `lo`, the upper two in `hi`.
+template <int FMT> __device__ __forceinline__ void to_half(uint32_t w, uint32_t &lo, uint32_t &hi) {
+  if constexpr (FMT == WNW_PAGES_E4M3) {
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(lo) : "h"((unsigned short)w));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(hi) : "h"((unsigned short)(w >> 16)));
+  } else {   // code + 128 as the low byte of an fp16 number between 1024 and 2048, less 1152: exact
+    w ^= 0x80808080u;
+    const uint32_t x = __byte_perm(w, 0x64646464u, 0x4140), y = __byte_perm(w, 0x64646464u, 0x4342), off = 0x64806480u;
+    const __half2 o = *reinterpret_cast<const __half2 *>(&off);
+    const __half2 p = __hsub2(*reinterpret_cast<const __half2 *>(&x), o), q = __hsub2(*reinterpret_cast<const __half2 *>(&y), o);
+    lo = *reinterpret_cast<const uint32_t *>(&p);
+    hi = *reinterpret_cast<const uint32_t *>(&q);
+  }
+}
+
+template <int D> struct Geo {
+  static constexpr int KC = D / 64;                    // 16-byte pieces of a K row that a lane takes
+  static constexpr int VB = D / 8;                     // bytes of a V row that a lane takes
+  static constexpr int MT = D / 16;                    // 16-row tiles of V^T
+  static constexpr int STAGE = 2 * PG_GR * D;          // bytes of a granule in the ring: K, then V
+  static constexpr int PITCH = D + 4;                  // floats of a row where the warps' results meet
+};
+template <int D, int NT> constexpr size_t smem_bytes() {
+  return (size_t)PA_WARPS * PA_STAGES * Geo<D>::STAGE + PA_WARPS * NT * 8 * Geo<D>::PITCH * 4 + PA_WARPS * NT * 8 * sizeof(PartRow) +
+         PA_WARPS * PA_STAGES * sizeof(float2) + PA_SEGS * sizeof(Seg) + (PG_MAX_SEQS + 1) * (sizeof(long long) + sizeof(int));
+}
+
+// The line: granules and heads (items) of the sequences before each one.  Returns the granules of all.
+template <int D>
+__device__ __forceinline__ long long lay_out(const AttendArgs &a, long long *grans, int *items) {
+  __shared__ long long wsum[PA_WARPS];
+  __shared__ long long isum[PA_WARPS];
+  const int n = a.bv.n_seqs, tid = threadIdx.x, lane = tid & 31, w = tid >> 5, cap = a.bv.stride * a.pv.T;
+  long long gbase = 0, ibase = 0;
+  for (int at = 0; at < n; at += PA_THREADS) {
+    const int s = at + tid;
+    long long gr = 0, it = 0;
+    if (s < n) {
+      int r0 = a.bv.starts[s], r1 = a.bv.starts[s + 1], len = a.bv.lengths[s];
+      if (r0 < 0 || r1 < r0 || r1 > a.bv.n_rows || len < 0 || len > cap) {
+        if (blockIdx.x == 0) pg_report(a.pv, WNW_PAGES_BAD_LENGTH);
+        r0 = max(r0, 0); r1 = min(r1, a.bv.n_rows); len = max(0, min(len, cap));
+      }
+      it = (long long)(r1 > r0 ? (r1 - r0 + a.rt - 1) / a.rt : 0) * a.pv.H;
+      gr = it * max(1, (len + PG_GR - 1) / PG_GR);      // (an empty sequence's rows are still to be written)
+    }
+    long long gi = gr, ii = it;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, gi, o), y = __shfl_up_sync(0xffffffffu, ii, o);
+      if (lane >= o) { gi += x; ii += y; }
+    }
+    if (lane == 31) { wsum[w] = gi; isum[w] = ii; }
+    __syncthreads();
+    long long gw = gbase, gt = 0, iw = ibase, itot = 0;
+#pragma unroll
+    for (int k = 0; k < PA_WARPS; ++k) {
+      if (k < w) { gw += wsum[k]; iw += isum[k]; }
+      gt += wsum[k];
+      itot += isum[k];
+    }
+    if (s < n) { grans[s] = gw + gi - gr; items[s] = (int)(iw + ii - it); }
+    gbase += gt;
+    ibase += itot;
+    __syncthreads();
+  }
+  if (tid == 0) { grans[n] = gbase; items[n] = (int)ibase; }
+  __syncthreads();
+  if (ibase > 1ll << 30) {             // (row starts that run over one another)
+    if (tid == 0 && blockIdx.x == 0) pg_report(a.pv, WNW_PAGES_BAD_LENGTH);
+    return 0;
+  }
+  return gbase;
+}
+// Granules that a CTA takes: equal stretches, none shorter than a granule for each warp.
+__device__ __forceinline__ long long stretch(long long total, int n_ctas) {
+  return max((long long)PA_WARPS, (total + n_ctas - 1) / n_ctas);
+}
+
+template <int D, int FMT, int NT>
+__global__ void __launch_bounds__(PA_THREADS, 1) wnw_pages_attend_kernel(const __grid_constant__ AttendArgs a) {
+  using G = Geo<D>;
+  extern __shared__ __align__(128) unsigned char smem[];
+  unsigned char *ring = smem;
+  float *meet = reinterpret_cast<float *>(ring + PA_WARPS * PA_STAGES * G::STAGE);            // [warp][row][PITCH]
+  PartRow *meet_row = reinterpret_cast<PartRow *>(meet + PA_WARPS * NT * 8 * G::PITCH);       // [warp][row]
+  float2 *ring_scale = reinterpret_cast<float2 *>(meet_row + PA_WARPS * NT * 8);              // [warp][stage]
+  Seg *segs = reinterpret_cast<Seg *>(ring_scale + PA_WARPS * PA_STAGES);
+  long long *grans = reinterpret_cast<long long *>(segs + PA_SEGS);
+  int *items = reinterpret_cast<int *>(grans + PG_MAX_SEQS + 1);
+
+  const PagesView &pv = a.pv;
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, c = lane & 3, r = lane >> 2;
+  const int gpp = pv.T / PG_GR;
+  const long long total = lay_out<D>(a, grans, items);
+  const long long len_line = stretch(total, gridDim.x), x0 = min(total, blockIdx.x * len_line), x1 = min(total, x0 + len_line);
+  if (tid == 0) a.part_head[blockIdx.x] = PartHead{0, 0};
+  if (x0 >= x1) return;
+  // the first head of the line
+  int item0 = 0;
+  {
+    int lo = 0, hi = a.bv.n_seqs;                       // the last sequence that begins at or before x0 and is not empty
+    while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (grans[mid] <= x0) lo = mid; else hi = mid; }
+    const int n_it = items[lo + 1] - items[lo];
+    const long long per = (grans[lo + 1] - grans[lo]) / n_it;
+    item0 = items[lo] + (int)((x0 - grans[lo]) / per);
+  }
+  const int n_items = items[a.bv.n_seqs];
+  const uint32_t ring_u = (uint32_t)__cvta_generic_to_shared(ring) + w * PA_STAGES * G::STAGE;
+
+  for (bool more = true; more;) {
+    // ---- the next stretches ----
+    __syncthreads();
+    int n_seg;
+    {
+      int mine = 0;
+      if (tid < PA_SEGS && item0 + tid < n_items) {
+        const int item = item0 + tid;
+        int lo = 0, hi = a.bv.n_seqs;
+        while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (items[mid] <= item) lo = mid; else hi = mid; }
+        const int n_it = items[lo + 1] - items[lo], it = item - items[lo], tiles = n_it / pv.H;
+        const long long per = (grans[lo + 1] - grans[lo]) / n_it, b = grans[lo] + it * per, e = b + per;
+        if (b < x1) {
+          mine = 1;
+          Seg &sg = segs[tid];
+          const long long f = max(b, x0), l = min(e, x1);
+          sg.s = lo; sg.h = it / tiles; sg.tile = it % tiles;
+          sg.g0 = (int)(f - b); sg.n = (int)(l - f); sg.y0 = (int)(f - x0);
+          const int cap = a.bv.stride * pv.T, r0 = max(a.bv.starts[lo], 0), r1 = min(a.bv.starts[lo + 1], a.bv.n_rows);
+          sg.len = max(0, min(a.bv.lengths[lo], cap));
+          sg.nq = min(a.rt, r1 - r0 - sg.tile * a.rt);
+          sg.row0 = r0 + sg.tile * a.rt;
+          sg.end0 = a.causal ? sg.len - (r1 - r0) + sg.tile * a.rt + 1 : sg.len;
+          const int last = min(sg.len, a.causal ? sg.end0 + sg.nq - 1 : sg.len);
+          sg.need = last > 0 ? (last + PG_GR - 1) / PG_GR : 0;
+          sg.item = item;
+          sg.slot = b >= x0 && e <= x1 ? -1 : b < x0 ? 0 : 1;
+          sg.n_parts = (int)((e - 1) / len_line - b / len_line + 1);
+        }
+      }
+      n_seg = __syncthreads_count(mine);
+    }
+    more = n_seg == PA_SEGS;                            // (a last round of none costs nothing)
+    item0 += n_seg;
+
+    // ---- copies run ahead of the products by PA_STAGES - 1 granules, over the stretches' ends ----
+    int p_seg = -1, p_g = 0, p_end = 0, p_cnt = 0, p_stage = 0;
+    long long p_off = 0;                                // lane i: where the stretch's granule 32 * k + i of this warp is
+    float p_k = 0.f, p_v = 0.f;
+    auto fetch = [&]() {
+      while (p_seg < n_seg && p_g >= p_end) {
+        if (++p_seg < n_seg) {
+          const Seg &sg = segs[p_seg];
+          p_g = sg.g0 + ((w - sg.y0) & (PA_WARPS - 1));
+          p_end = min(sg.g0 + sg.n, sg.need);
+          p_cnt = 0;
+        }
+      }
+      if (p_seg < n_seg) {
+        const Seg &sg = segs[p_seg];
+        if ((p_cnt & 31) == 0) {
+          const int g = p_g + PA_WARPS * lane;
+          p_off = 0;
+          p_k = -1.f;                                   // a page that is not there: nothing of it is seen
+          p_v = 0.f;
+          if (g < p_end) {
+            const int page = a.bv.table[(long long)sg.s * a.bv.stride + g / gpp];
+            if (page >= 0 && page < pv.n_pages) {
+              p_off = page * pv.page_stride + (long long)sg.h * 2 * pv.T * D + (g % gpp) * PG_GR * D;
+              const float *sc = pv.scales + page * pv.scale_stride + sg.h * 2;
+              p_k = fabsf(sc[0]);
+              p_v = sc[1];
+            } else {
+              pg_report(pv, WNW_PAGES_BAD_PAGE);
+            }
+          }
+        }
+        const int j = p_cnt & 31;
+        const long long off = __shfl_sync(0xffffffffu, p_off, j);
+        const float ks = __shfl_sync(0xffffffffu, p_k, j), vs = __shfl_sync(0xffffffffu, p_v, j);
+        if (lane == 0) ring_scale[w * PA_STAGES + p_stage] = make_float2(ks, vs);
+        const unsigned char *kp = pv.codes + off, *vp = kp + (long long)pv.T * D;
+        const uint32_t dst = ring_u + p_stage * G::STAGE;
+        const int left = ks < 0.f ? 0 : sg.len - p_g * PG_GR;         // rows of the granule that exist
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int k = 0; k < G::KC; ++k) {
+            const int row = r + 8 * t;
+            copy_async<16>(dst + (t * G::KC + k) * 512 + lane * 16, kp + row * D + 64 * k + 16 * c, row < left);
+          }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int row = 2 * c + (t & 1) + 8 * (t >> 1);
+          copy_async<G::VB>(dst + PG_GR * D + t * 32 * G::VB + lane * G::VB, vp + row * D + G::VB * r, row < left);
+        }
+        p_g += PA_WARPS;
+        ++p_cnt;
+        if (++p_stage == PA_STAGES) p_stage = 0;
+      }
+      asm volatile("cp.async.commit_group;\n" ::: "memory");
+    };
+#pragma unroll
+    for (int k = 0; k < PA_STAGES - 1; ++k) fetch();
+
+    int stage = 0;
+    for (int si = 0; si < n_seg; ++si) {
+      const Seg sg = segs[si];
+      // ---- the query rows: lane (r, c) holds row r of each tile of eight, the head_dim elements of its K bytes ----
+      uint32_t qf[NT][G::KC * 8];
+      float f_col[NT][2];                               // log2 scale of the scores' two columns 2c, 2c + 1
+      int end_col[NT][2];                               // tokens that those rows see
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int j = t * 8 + r, tok = j / a.g, hd = j - tok * a.g;
+        const bool real = j < a.rt * a.g && tok < sg.nq;
+        uint4 raw[G::KC * 2];
+#pragma unroll
+        for (int k = 0; k < G::KC * 2; ++k) raw[k] = make_uint4(0, 0, 0, 0);
+        if (real) {
+          const unsigned char *p = a.q.p + 2 * ((long long)(sg.row0 + tok) * a.q.row + (sg.h * a.g + hd) * a.q.head);
+#pragma unroll
+          for (int k = 0; k < G::KC; ++k) {
+            raw[2 * k] = *reinterpret_cast<const uint4 *>(p + 2 * (64 * k + 16 * c));
+            raw[2 * k + 1] = *reinterpret_cast<const uint4 *>(p + 2 * (64 * k + 16 * c) + 16);
+          }
+        }
+        float most = 0.f;
+        float2 x[G::KC * 8];
+#pragma unroll
+        for (int k = 0; k < G::KC * 2; ++k) {
+          const uint32_t u[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+#pragma unroll
+          for (int z = 0; z < 4; ++z) {
+            x[4 * k + z] = a.dtype == WNW_DTYPE_BF16 ? Pair<__nv_bfloat16>::get(u[z]) : Pair<__half>::get(u[z]);
+            most = fmaxf(most, fmaxf(fabsf(x[4 * k + z].x), fabsf(x[4 * k + z].y)));
+          }
+        }
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        // largest magnitude into [2^14, 2^15); rows of zeros and with infinities as they are
+        const int eq = most > 0.f && most < INFINITY ? max(-100, (int)(__float_as_uint(most) >> 23) - 127 - 14) : 0;
+        const float down = __uint_as_float((uint32_t)(127 - eq) << 23);
+#pragma unroll
+        for (int k = 0; k < G::KC * 8; ++k) qf[t][k] = half2_of(x[k].x * down, x[k].y * down);
+        const float up = a.scale_log2 * __uint_as_float((uint32_t)(eq + 127) << 23);
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          f_col[t][z] = __shfl_sync(0xffffffffu, up, (2 * c + z) * 4);
+          const int jc = t * 8 + 2 * c + z;
+          end_col[t][z] = a.causal ? min(sg.len, sg.end0 + jc / a.g) : sg.len;
+        }
+      }
+      const int end_min = a.causal ? sg.end0 : sg.len;   // up to here every row of the tile sees every token
+
+      float o[NT][G::MT][4], m[NT][2], big_m[NT][2], l[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int i = 0; i < G::MT; ++i) o[t][i][0] = o[t][i][1] = o[t][i][2] = o[t][i][3] = 0.f;
+        m[t][0] = m[t][1] = big_m[t][0] = big_m[t][1] = -INFINITY;
+        l[t][0] = l[t][1] = 0.f;
+      }
+
+      const int g_end = min(sg.g0 + sg.n, sg.need);
+      for (int g = sg.g0 + ((w - sg.y0) & (PA_WARPS - 1)); g < g_end; g += PA_WARPS) {
+        __syncwarp();
+        fetch();
+        asm volatile("cp.async.wait_group %0;\n" ::"n"(PA_STAGES - 1) : "memory");
+        __syncwarp();
+        const float2 sc = ring_scale[w * PA_STAGES + stage];
+        const unsigned char *src = ring + (w * PA_STAGES + stage) * G::STAGE;
+        if (++stage == PA_STAGES) stage = 0;
+        // S^T: tokens r, r + 8 x columns 2c, 2c + 1
+        float s[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+#pragma unroll
+        for (int k = 0; k < G::KC; ++k) {
+          const uint4 u = *reinterpret_cast<const uint4 *>(src + k * 512 + lane * 16), v = *reinterpret_cast<const uint4 *>(src + (G::KC + k) * 512 + lane * 16);
+          const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, vw[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int z = 0; z < 4; ++z) {
+            uint32_t a0, a1, a2, a3;
+            to_half<FMT>(uw[z], a0, a2);
+            to_half<FMT>(vw[z], a1, a3);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma(s[t], a0, a1, a2, a3, qf[t][8 * k + 2 * z], qf[t][8 * k + 2 * z + 1]);
+          }
+        }
+        const int tok = g * PG_GR + r;
+        const bool partly = sc.x < 0.f || (g + 1) * PG_GR > end_min;
+        const float e_v = (float)((int)(__float_as_uint(sc.y) >> 23 & 255) - 127);
+        uint32_t pb[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const float f0 = f_col[t][0] * sc.x, f1 = f_col[t][1] * sc.x;
+          s[t][0] *= f0; s[t][1] *= f1; s[t][2] *= f0; s[t][3] *= f1;
+          if (partly) {
+            const bool there = sc.x >= 0.f;
+            if (!there || tok >= end_col[t][0]) s[t][0] = -INFINITY;
+            if (!there || tok >= end_col[t][1]) s[t][1] = -INFINITY;
+            if (!there || tok + 8 >= end_col[t][0]) s[t][2] = -INFINITY;
+            if (!there || tok + 8 >= end_col[t][1]) s[t][3] = -INFINITY;
+          }
+          float top0 = fmaxf(s[t][0], s[t][2]), top1 = fmaxf(s[t][1], s[t][3]);
+          const bool far = top0 > m[t][0] + LAZY || top1 > m[t][1] + LAZY || top0 + e_v > big_m[t][0] + LAZY || top1 + e_v > big_m[t][1] + LAZY;
+          if (__any_sync(0xffffffffu, far)) {
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) {
+              top0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, x));
+              top1 = fmaxf(top1, __shfl_xor_sync(0xffffffffu, top1, x));
+            }
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+              const float top = z ? top1 : top0, mn = fmaxf(m[t][z], top), bn = fmaxf(big_m[t][z], top + e_v);
+              // (-inf: nothing has been seen, the sums are zero)
+              l[t][z] *= m[t][z] == -INFINITY ? 1.f : ex2(m[t][z] - mn);
+              const float by = big_m[t][z] == -INFINITY ? 1.f : ex2(big_m[t][z] - bn);
+#pragma unroll
+              for (int i = 0; i < G::MT; ++i) { o[t][i][z] *= by; o[t][i][2 + z] *= by; }
+              m[t][z] = mn;
+              big_m[t][z] = bn;
+            }
+          }
+          const float m0 = m[t][0] == -INFINITY ? 0.f : m[t][0], m1 = m[t][1] == -INFINITY ? 0.f : m[t][1];
+          // (finite: where the scales are that far apart, p is zero)
+          const float w0 = big_m[t][0] == -INFINITY ? 0.f : ex2(fminf(m0 + e_v - big_m[t][0], 126.f));
+          const float w1 = big_m[t][1] == -INFINITY ? 0.f : ex2(fminf(m1 + e_v - big_m[t][1], 126.f));
+          const float p0 = ex2(s[t][0] - m0), p1 = ex2(s[t][1] - m1), p2 = ex2(s[t][2] - m0), p3 = ex2(s[t][3] - m1);
+          l[t][0] += p0 + p2;
+          l[t][1] += p1 + p3;
+          pb[t][0] = transposed(half2_of(p0 * w0, p1 * w1));
+          pb[t][1] = transposed(half2_of(p2 * w0, p3 * w1));
+        }
+        // O^T: elements VB * r + 2i (c0, c1) and VB * r + 2i + 1 (c2, c3) of the columns 2c, 2c + 1
+        uint32_t vw[4][G::VB / 4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const unsigned char *p = src + PG_GR * D + t * 32 * G::VB + lane * G::VB;
+          if constexpr (G::VB == 16) { const uint4 u = *reinterpret_cast<const uint4 *>(p); vw[t][0] = u.x; vw[t][1] = u.y; vw[t][2] = u.z; vw[t][3] = u.w; }
+          else { const uint2 u = *reinterpret_cast<const uint2 *>(p); vw[t][0] = u.x; vw[t][1] = u.y; }
+        }
+        bool nan_codes = false;                          // in a granule that some rows see only part of
+        if (FMT == WNW_PAGES_E4M3 && partly && a.causal && sg.nq > 1) {
+          bool mine = false;
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int z = 0; z < G::VB / 4; ++z) mine |= __vcmpeq4(vw[t][z] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
+          nan_codes = __any_sync(0xffffffffu, mine);
+        }
+        if (!nan_codes) {
+#pragma unroll
+          for (int z = 0; z < G::VB / 4; ++z) {
+            uint32_t x0, x1, x2, x3, y0, y1, y2, y3;
+            to_half<FMT>(__byte_perm(vw[0][z], vw[1][z], 0x5140), x0, x1);
+            to_half<FMT>(__byte_perm(vw[2][z], vw[3][z], 0x5140), x2, x3);
+            to_half<FMT>(__byte_perm(vw[0][z], vw[1][z], 0x7362), y0, y1);
+            to_half<FMT>(__byte_perm(vw[2][z], vw[3][z], 0x7362), y2, y3);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              mma(o[t][2 * z], x0, x1, x2, x3, pb[t][0], pb[t][1]);
+              mma(o[t][2 * z + 1], y0, y1, y2, y3, pb[t][0], pb[t][1]);
+            }
+          }
+        } else {
+          // a weight of zero does not keep a not-a-number out: they are taken out of the product, and counted for the rows that see them
+#pragma unroll
+          for (int z = 0; z < G::VB / 4; ++z) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              uint32_t x[4], bad[4];
+              to_half<FMT>(__byte_perm(vw[0][z], vw[1][z], half ? 0x7362 : 0x5140), x[0], x[1]);
+              to_half<FMT>(__byte_perm(vw[2][z], vw[3][z], half ? 0x7362 : 0x5140), x[2], x[3]);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const __half2 h = *reinterpret_cast<const __half2 *>(&x[k]);
+                const bool b0 = __hisnan(__low2half(h)), b1 = __hisnan(__high2half(h));
+                bad[k] = (b0 ? 0x3c00u : 0u) | (b1 ? 0x3c000000u : 0u);
+                x[k] &= (b0 ? 0u : 0xffffu) | (b1 ? 0u : 0xffff0000u);
+              }
+#pragma unroll
+              for (int t = 0; t < NT; ++t) {
+                const int end = min(sg.len, sg.end0 + (t * 8 + r) / a.g), t0 = g * PG_GR + 2 * c;    // of column r: the lane's part of P^T
+                const uint32_t see0 = (t0 < end ? 0x3c00u : 0u) | (t0 + 1 < end ? 0x3c000000u : 0u);
+                const uint32_t see1 = (t0 + 8 < end ? 0x3c00u : 0u) | (t0 + 9 < end ? 0x3c000000u : 0u);
+                float n[4] = {0.f, 0.f, 0.f, 0.f};
+                mma(o[t][2 * z + half], x[0], x[1], x[2], x[3], pb[t][0], pb[t][1]);
+                mma(n, bad[0], bad[1], bad[2], bad[3], see0, see1);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  if (n[k] > 0.f) o[t][2 * z + half][k] = NAN;
+              }
+            }
+          }
+        }
+      }
+
+      // ---- the warps' results meet ----
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) l[t][z] += __shfl_xor_sync(0xffffffffu, l[t][z], x);
+          float *p = meet + ((w * NT + t) * 8 + 2 * c + z) * G::PITCH + G::VB * r;
+#pragma unroll
+          for (int i = 0; i < G::MT; i += 2) *reinterpret_cast<float4 *>(p + 2 * i) = make_float4(o[t][i][z], o[t][i][2 + z], o[t][i + 1][z], o[t][i + 1][2 + z]);
+          if (r == 0) meet_row[(w * NT + t) * 8 + 2 * c + z] = PartRow{m[t][z], big_m[t][z], l[t][z], 0.f};
+        }
+      __syncthreads();
+      for (int i = tid; i < NT * 8 * (D / 4); i += PA_THREADS) {
+        const int j = i / (D / 4), d = i % (D / 4) * 4, tok = j / a.g, hd = j - tok * a.g;
+        if (j < a.rt * a.g && tok < sg.nq) {
+          float mx = -INFINITY, bx = -INFINITY;
+#pragma unroll
+          for (int k = 0; k < PA_WARPS; ++k) {
+            mx = fmaxf(mx, meet_row[k * NT * 8 + j].m);
+            bx = fmaxf(bx, meet_row[k * NT * 8 + j].big_m);
+          }
+          float sum = 0.f;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (mx != -INFINITY) {
+#pragma unroll
+            for (int k = 0; k < PA_WARPS; ++k) {
+              const PartRow pr = meet_row[k * NT * 8 + j];
+              const float4 x = *reinterpret_cast<const float4 *>(meet + (k * NT * 8 + j) * G::PITCH + d);
+              const float by = ex2(pr.big_m - bx);
+              sum += pr.l * ex2(pr.m - mx);
+              acc.x += x.x * by; acc.y += x.y * by; acc.z += x.z * by; acc.w += x.w * by;
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < PA_WARPS; ++k) sum += meet_row[k * NT * 8 + j].l;     // 0, or not-a-number where a score was none
+          }
+          if (sg.slot < 0) {
+            const float by = sum == 0.f ? 0.f : (mx == -INFINITY ? sum : ex2(bx - mx) / sum);
+            const long long row = sg.row0 + tok;
+            const int head = sg.h * a.g + hd;
+            unsigned char *p = a.out.p + 2 * (row * a.out.row + head * a.out.head + d);
+            uint2 v;
+            if (a.dtype == WNW_DTYPE_BF16) v = make_uint2(Pair<__nv_bfloat16>::put(acc.x * by, acc.y * by), Pair<__nv_bfloat16>::put(acc.z * by, acc.w * by));
+            else v = make_uint2(Pair<__half>::put(acc.x * by, acc.y * by), Pair<__half>::put(acc.z * by, acc.w * by));
+            *reinterpret_cast<uint2 *>(p) = v;
+            if (a.lse && d == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx == -INFINITY ? sum : (mx + log2f(sum)) * 0.69314718055994531f);
+          } else {
+            const long long at = ((long long)blockIdx.x * 2 + sg.slot) * PA_ROWS + j;
+            *reinterpret_cast<float4 *>(a.part_o + at * D + d) = acc;
+            if (d == 0) a.part_row[at] = PartRow{mx, bx, sum, 0.f};
+          }
+        }
+      }
+      if (tid == 0 && sg.slot == 1) a.part_head[blockIdx.x] = PartHead{sg.item, sg.n_parts};
+      __syncthreads();
+    }
+    asm volatile("cp.async.wait_all;\n" ::: "memory");
+  }
+}
+
+// A head that several CTAs share: CTA (b, j) puts row j of the head together that begins in CTA b of the attention and does not end there.
+template <int D>
+__global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr int LANES = D / 4, SPLIT = 128 / LANES;
+  __shared__ float4 acc_s[SPLIT][LANES];
+  __shared__ float sum_s[SPLIT];
+  const PartHead ph = a.part_head[blockIdx.x];
+  const int j = blockIdx.y, tok = j / a.g, hd = j - tok * a.g;
+  if (ph.n_parts < 2) return;
+  // which rows: the item's sequence again
+  int s = 0, base = 0, tiles = 0, r0 = 0, r1 = 0;
+  for (; s < a.bv.n_seqs; ++s) {
+    r0 = max(a.bv.starts[s], 0);
+    r1 = min(a.bv.starts[s + 1], a.bv.n_rows);
+    tiles = r1 > r0 ? (r1 - r0 + a.rt - 1) / a.rt : 0;
+    if (ph.item < base + tiles * a.pv.H) break;
+    base += tiles * a.pv.H;
+  }
+  if (s == a.bv.n_seqs) return;
+  const int it = ph.item - base, h = it / tiles, tile = it % tiles, nq = min(a.rt, r1 - r0 - tile * a.rt);
+  if (tok >= nq) return;
+  const int part = threadIdx.x / LANES, d = threadIdx.x % LANES;
+  auto at = [&](int k) { return ((long long)(blockIdx.x + k) * 2 + (k == 0)) * PA_ROWS + j; };
+  float mx = -INFINITY, bx = -INFINITY;
+  for (int k = threadIdx.x; k < ph.n_parts; k += 128) {
+    const PartRow pr = a.part_row[at(k)];
+    mx = fmaxf(mx, pr.m);
+    bx = fmaxf(bx, pr.big_m);
+  }
+  __shared__ float red[2][4];
+#pragma unroll
+  for (int x = 16; x; x >>= 1) {
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+    bx = fmaxf(bx, __shfl_xor_sync(0xffffffffu, bx, x));
+  }
+  if ((threadIdx.x & 31) == 0) { red[0][threadIdx.x >> 5] = mx; red[1][threadIdx.x >> 5] = bx; }
+  __syncthreads();
+  mx = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  bx = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float sum = 0.f;
+#pragma unroll 4
+  for (int k = part; k < ph.n_parts; k += SPLIT) {
+    const PartRow pr = a.part_row[at(k)];
+    const float4 x = *reinterpret_cast<const float4 *>(a.part_o + at(k) * D + 4 * d);
+    const float by = mx == -INFINITY ? 0.f : ex2(pr.big_m - bx);
+    sum += mx == -INFINITY ? pr.l : pr.l * ex2(pr.m - mx);
+    acc.x += x.x * by; acc.y += x.y * by; acc.z += x.z * by; acc.w += x.w * by;
+  }
+  acc_s[part][d] = acc;
+  if (d == 0) sum_s[part] = sum;
+  __syncthreads();
+  if (part) return;
+  sum = 0.f;
+  acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int k = 0; k < SPLIT; ++k) {
+    const float4 x = acc_s[k][d];
+    sum += sum_s[k];
+    acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+  }
+  const float by = sum == 0.f ? 0.f : (mx == -INFINITY ? sum : ex2(bx - mx) / sum);
+  const long long row = r0 + tile * a.rt + tok;
+  const int head = h * a.g + hd;
+  unsigned char *p = a.out.p + 2 * (row * a.out.row + head * a.out.head + 4 * d);
+  if (a.dtype == WNW_DTYPE_BF16) *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__nv_bfloat16>::put(acc.x * by, acc.y * by), Pair<__nv_bfloat16>::put(acc.z * by, acc.w * by));
+  else *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__half>::put(acc.x * by, acc.y * by), Pair<__half>::put(acc.z * by, acc.w * by));
+  if (a.lse && d == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx == -INFINITY ? sum : (mx + log2f(sum)) * 0.69314718055994531f);
+}
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+size_t workspace_bytes(int n_ctas, int d, size_t *rows, size_t *heads) {
+  *rows = align256((size_t)n_ctas * 2 * PA_ROWS * d * sizeof(float));
+  *heads = *rows + align256((size_t)n_ctas * 2 * PA_ROWS * sizeof(PartRow));
+  return *heads + align256((size_t)n_ctas * sizeof(PartHead));
+}
+
+template <int D, int FMT, int NT> cudaError_t launch(const AttendArgs &a, int n_ctas, int device, cudaStream_t st) {
+  static std::atomic<unsigned long long> ready{0};       // devices whose kernel has its shared memory
+  if (!(ready.load(std::memory_order_acquire) >> device & 1)) {
+    const cudaError_t e = cudaFuncSetAttribute(wnw_pages_attend_kernel<D, FMT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D, NT>());
+    if (e != cudaSuccess) return e;
+    ready.fetch_or(1ull << device, std::memory_order_release);
+  }
+  wnw_pages_attend_kernel<D, FMT, NT><<<n_ctas, PA_THREADS, smem_bytes<D, NT>(), st>>>(a);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  wnw_pages_join_kernel<D><<<dim3(n_ctas, a.rt * a.g), 128, 0, st>>>(a);
+  return cudaGetLastError();
+}
+template <int D, int FMT> cudaError_t launch(const AttendArgs &a, int nt, int n_ctas, int device, cudaStream_t st) {
+  return nt == 1 ? launch<D, FMT, 1>(a, n_ctas, device, st) : launch<D, FMT, 2>(a, n_ctas, device, st);
+}
+
+wnw_status_t check_heads(const wnw_pages_t *p, int n_q_heads) {
+  if (n_q_heads < 1 || n_q_heads % p->n_kv_heads) return WNW_ERR_INVALID_ARG;
+  return n_q_heads / p->n_kv_heads > 16 ? WNW_ERR_UNSUPPORTED : WNW_OK;
+}
+
+}  // namespace
+}  // namespace wnw
+
+using namespace wnw;
+
+extern "C" wnw_status_t wnw_pages_attend_workspace(const wnw_pages_t *pages, int32_t n_q_heads, int64_t *bytes) {
+  PagesView pv;
+  wnw_status_t rc = pg_view(pages, &pv);
+  if (rc != WNW_OK || !bytes) return rc != WNW_OK ? rc : WNW_ERR_INVALID_ARG;
+  if ((rc = check_heads(pages, n_q_heads)) != WNW_OK) return rc;
+  OnDevice on(pages->device);
+  int n_sm = 0;
+  if (!on.ok || pg_sms(pages->device, &n_sm) != WNW_OK) return WNW_ERR_CUDA;
+  size_t r, h;
+  *bytes = (int64_t)workspace_bytes(n_sm, pages->head_dim, &r, &h);
+  return WNW_OK;
+}
+
+extern "C" wnw_status_t wnw_pages_attend(const wnw_pages_t *pages, const wnw_batch_t *batch, const wnw_rows_t *q, const wnw_rows_t *out,
+                                         float *lse_dev, int32_t dtype, int32_t causal, float softmax_scale, void *workspace_dev,
+                                         int64_t workspace_size, void *cuda_stream) {
+  AttendArgs a;
+  memset(&a, 0, sizeof(a));
+  wnw_status_t rc = pg_view(pages, batch, &a.pv, &a.bv);
+  if (rc != WNW_OK) return rc;
+  if (!q || !out || (causal & ~1) || q->n_heads != out->n_heads || !(softmax_scale >= 0.f) || std::isinf(softmax_scale)) return WNW_ERR_INVALID_ARG;
+  if (dtype != WNW_DTYPE_BF16 && dtype != WNW_DTYPE_FP16) return WNW_ERR_UNSUPPORTED;
+  if ((rc = check_heads(pages, q->n_heads)) != WNW_OK) return rc;
+  if (!batch->n_seqs || !batch->n_rows) return WNW_OK;
+  if (!q->dev || !out->dev || !pg_vector_rows(*q, dtype) || !pg_vector_rows(*out, dtype) || (uintptr_t)lse_dev % 4) return WNW_ERR_INVALID_ARG;
+  OnDevice on(pages->device);
+  int n_sm = 0;
+  if (!on.ok || pg_sms(pages->device, &n_sm) != WNW_OK) return WNW_ERR_CUDA;
+  size_t rows_at, heads_at;
+  const size_t need = workspace_bytes(n_sm, pages->head_dim, &rows_at, &heads_at);
+  if (!workspace_dev || (uintptr_t)workspace_dev % 256 || workspace_size < (int64_t)need) return WNW_ERR_INVALID_ARG;
+  a.q = rows_view(*q);
+  a.out = rows_view(*out);
+  a.lse = lse_dev;
+  a.Hq = q->n_heads;
+  a.g = q->n_heads / pages->n_kv_heads;
+  a.dtype = dtype;
+  a.causal = causal;
+  a.scale_log2 = (float)((softmax_scale > 0.f ? (double)softmax_scale : 1.0 / std::sqrt((double)pages->head_dim)) * 1.4426950408889634);
+  a.part_o = (float *)workspace_dev;
+  a.part_row = (PartRow *)((char *)workspace_dev + rows_at);
+  a.part_head = (PartHead *)((char *)workspace_dev + heads_at);
+  const int max_rows = batch->max_rows > 0 ? std::min(batch->max_rows, batch->n_rows) : batch->n_rows;
+  const int nt = (long long)max_rows * a.g <= 8 ? 1 : 2;
+  a.rt = std::min(nt * 8 / a.g, max_rows);
+  // items are counted in 32 bits
+  if (((long long)batch->n_rows / a.rt + batch->n_seqs) * pages->n_kv_heads > 1ll << 30) return WNW_ERR_CAPACITY;
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  cudaError_t e;
+  if (pages->head_dim == 64) e = pages->format == WNW_PAGES_E4M3 ? launch<64, WNW_PAGES_E4M3>(a, nt, n_sm, pages->device, st) : launch<64, WNW_PAGES_INT8>(a, nt, n_sm, pages->device, st);
+  else e = pages->format == WNW_PAGES_E4M3 ? launch<128, WNW_PAGES_E4M3>(a, nt, n_sm, pages->device, st) : launch<128, WNW_PAGES_INT8>(a, nt, n_sm, pages->device, st);
+  return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
+}

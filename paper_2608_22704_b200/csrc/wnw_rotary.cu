@@ -1,0 +1,210 @@
+// wnw_rotate: rotary positions with several axes, forward and inverse, for the queries and keys of a layer in one launch.
+//
+// (a, b) -> (a cos t - b sin t, b cos t + a sin t), t = positions[axis of the pair][token] * frequency of the pair.  Every element is
+// read and written once, so memory bounds it from some thousand tokens on, a launch below that.  The angles of a token are shared by
+// all heads: a CTA takes a few tokens, leaves their cosines and sines in shared memory, one thread a pair, and then goes over the
+// heads' rows 16 bytes at a time.
+#include <algorithm>
+#include <cstring>
+
+#include "wnw_pages.cuh"
+
+namespace wnw {
+namespace {
+
+constexpr int ROT_THREADS = 256;
+
+struct RotateArgs {
+  RotaryView rot;
+  RowsView in[2], out[2];            // queries, keys
+  int n_heads[2];
+  const int32_t *positions;
+  long long axis_stride;
+  int n_tokens, head_dim, tokens_per_cta, tail;   // tail: elements behind the pairs that have to be copied
+};
+
+template <typename T> struct Elems;
+template <> struct Elems<float> {
+  static __device__ __forceinline__ float get(const float *p) { return *p; }
+  static __device__ __forceinline__ void put(float *p, float x) { *p = x; }
+};
+template <> struct Elems<__nv_bfloat16> {
+  static __device__ __forceinline__ float get(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+  static __device__ __forceinline__ void put(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
+};
+template <> struct Elems<__half> {
+  static __device__ __forceinline__ float get(const __half *p) { return __half2float(*p); }
+  static __device__ __forceinline__ void put(__half *p, float x) { *p = __float2half_rn(x); }
+};
+
+// 16 bytes as floats and back
+template <typename T> struct Vec {
+  static constexpr int N = 8;
+  float x[8];
+  __device__ __forceinline__ void get(uint4 u) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { const float2 f = Pair<T>::get(w[i]); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
+  }
+  __device__ __forceinline__ uint4 put() const {
+    return make_uint4(Pair<T>::put(x[0], x[1]), Pair<T>::put(x[2], x[3]), Pair<T>::put(x[4], x[5]), Pair<T>::put(x[6], x[7]));
+  }
+};
+template <> struct Vec<float> {
+  static constexpr int N = 4;
+  float x[4];
+  __device__ __forceinline__ void get(uint4 u) { x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y); x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w); }
+  __device__ __forceinline__ uint4 put() const { return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])); }
+};
+
+// A unit of work is N pairs of one head and token: two vectors of 16 bytes (VEC), or one pair.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(ROT_THREADS) wnw_rotate_kernel(const __grid_constant__ RotateArgs a) {
+  extern __shared__ float2 cs[];                        // [tokens_per_cta][n_pairs]
+  const int np = a.rot.n_pairs, t0 = blockIdx.x * a.tokens_per_cta, nt = min(a.tokens_per_cta, a.n_tokens - t0);
+  for (int i = threadIdx.x; i < nt * np; i += ROT_THREADS) {
+    const int t = i / np, p = i - t * np;
+    cs[i] = pg_angle(a.rot, p, a.positions[a.rot.axis[p] * a.axis_stride + t0 + t]);
+  }
+  __syncthreads();
+  constexpr int N = VEC ? Vec<T>::N : 1;
+  const int units = np / N, heads = a.n_heads[0] + a.n_heads[1], all = nt * heads * units;
+  for (int i = threadIdx.x; i < all; i += ROT_THREADS) {
+    const int row = i / units, u = i - row * units, t = row / heads, h0 = row - t * heads;
+    const int which = h0 >= a.n_heads[0], h = h0 - (which ? a.n_heads[0] : 0);
+    const T *in = reinterpret_cast<const T *>(a.in[which].p) + (t0 + t) * a.in[which].row + h * a.in[which].head;
+    T *out = reinterpret_cast<T *>(a.out[which].p) + (t0 + t) * a.out[which].row + h * a.out[which].head;
+    const float2 *c = cs + t * np + u * N;
+    const int lo = a.rot.neighbours ? 2 * N * u : N * u, hi = a.rot.neighbours ? lo + N : N * u + np;
+    if constexpr (VEC) {
+      Vec<T> x, y;
+      x.get(*reinterpret_cast<const uint4 *>(in + lo));
+      y.get(*reinterpret_cast<const uint4 *>(in + hi));
+      if (a.rot.neighbours) {
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) {
+          const float2 s = pg_turn(x.x[2 * j], x.x[2 * j + 1], c[j]), t = pg_turn(y.x[2 * j], y.x[2 * j + 1], c[N / 2 + j]);
+          x.x[2 * j] = s.x; x.x[2 * j + 1] = s.y;
+          y.x[2 * j] = t.x; y.x[2 * j + 1] = t.y;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float2 s = pg_turn(x.x[j], y.x[j], c[j]);
+          x.x[j] = s.x; y.x[j] = s.y;
+        }
+      }
+      *reinterpret_cast<uint4 *>(out + lo) = x.put();
+      *reinterpret_cast<uint4 *>(out + hi) = y.put();
+    } else {
+      const float2 s = pg_turn(Elems<T>::get(in + lo), Elems<T>::get(in + hi), c[0]);
+      Elems<T>::put(out + lo, s.x);
+      Elems<T>::put(out + hi, s.y);
+    }
+  }
+  if (a.tail) {                                          // what the pairs leave, where the output is another tensor
+    const int all_tail = nt * heads * a.tail;
+    for (int i = threadIdx.x; i < all_tail; i += ROT_THREADS) {
+      const int row = i / a.tail, e = 2 * np + i - row * a.tail, t = row / heads, h0 = row - t * heads;
+      const int which = h0 >= a.n_heads[0], h = h0 - (which ? a.n_heads[0] : 0);
+      const RowsView &in = a.in[which], &out = a.out[which];
+      reinterpret_cast<T *>(out.p)[(t0 + t) * out.row + h * out.head + e] = reinterpret_cast<const T *>(in.p)[(t0 + t) * in.row + h * in.head + e];
+    }
+  }
+}
+
+template <typename T> cudaError_t launch(const RotateArgs &a, bool vec, cudaStream_t st) {
+  const int grid = (a.n_tokens + a.tokens_per_cta - 1) / a.tokens_per_cta;
+  const size_t smem = sizeof(float2) * a.tokens_per_cta * a.rot.n_pairs;
+  if (vec) wnw_rotate_kernel<T, true><<<grid, ROT_THREADS, smem, st>>>(a);
+  else wnw_rotate_kernel<T, false><<<grid, ROT_THREADS, smem, st>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+wnw_status_t rotary_view(const wnw_rotary_t *r, int head_dim, int inverse, RotaryView *v) {
+  if (r->n_pairs < 1 || r->n_pairs > 128 || r->n_axes < 1 || r->n_axes > 4 || (r->neighbours & ~1) || 2 * r->n_pairs > head_dim) return WNW_ERR_INVALID_ARG;
+  memset(v, 0, sizeof(*v));
+  for (int i = 0; i < r->n_pairs; ++i) {
+    if (r->axis[i] >= r->n_axes || !std::isfinite(r->frequency[i])) return WNW_ERR_INVALID_ARG;
+    v->turns[i] = r->frequency[i] / 6.283185307179586476925286766559;
+    v->axis[i] = r->axis[i];
+  }
+  v->n_pairs = r->n_pairs;
+  v->neighbours = r->neighbours;
+  v->sign = inverse ? -1.f : 1.f;
+  return WNW_OK;
+}
+
+}  // namespace wnw
+
+using namespace wnw;
+
+extern "C" wnw_status_t wnw_rotary_init(wnw_rotary_t *rotary, int32_t n_pairs, double base, const int32_t *sections, int32_t n_axes,
+                                        int32_t dealt, int32_t neighbours) {
+  if (!rotary || !sections || n_pairs < 1 || n_pairs > 128 || n_axes < 1 || n_axes > 4 || !(base > 0) || !std::isfinite(base)) return WNW_ERR_INVALID_ARG;
+  if ((dealt & ~1) || (neighbours & ~1)) return WNW_ERR_INVALID_ARG;
+  long long sum = 0;
+  for (int a = 0; a < n_axes; ++a) {
+    if (sections[a] < 0) return WNW_ERR_INVALID_ARG;
+    sum += sections[a];
+  }
+  if (sum != n_pairs) return WNW_ERR_INVALID_ARG;
+  wnw_rotary_t r;
+  memset(&r, 0, sizeof(r));
+  r.n_pairs = n_pairs;
+  r.n_axes = n_axes;
+  r.neighbours = neighbours;
+  for (int i = 0, a = 0, left = sections[0]; i < n_pairs; ++i) {
+    r.frequency[i] = std::pow(base, -(double)i / n_pairs);
+    if (dealt) {
+      r.axis[i] = (uint8_t)(i / n_axes < sections[i % n_axes] ? i % n_axes : 0);
+    } else {
+      while (left == 0) left = sections[++a];
+      --left;
+      r.axis[i] = (uint8_t)a;
+    }
+  }
+  *rotary = r;
+  return WNW_OK;
+}
+
+extern "C" wnw_status_t wnw_rotate(const wnw_rotary_t *rotary, const int32_t *positions_dev, int64_t axis_stride, int32_t n_tokens,
+                                   int32_t head_dim, int32_t dtype, const wnw_rows_t *q, const wnw_rows_t *q_out, const wnw_rows_t *k,
+                                   const wnw_rows_t *k_out, int32_t inverse, int32_t device, void *cuda_stream) {
+  if (!rotary || !q || !q_out || !k != !k_out || n_tokens < 0 || (inverse & ~1)) return WNW_ERR_INVALID_ARG;
+  if (head_dim < 2 || head_dim > 256 || head_dim % 2 || dtype < WNW_DTYPE_BF16 || dtype > WNW_DTYPE_FP32) return WNW_ERR_UNSUPPORTED;
+  RotateArgs a;
+  const wnw_status_t rc = rotary_view(rotary, head_dim, inverse, &a.rot);
+  if (rc != WNW_OK) return rc;
+  const int size = (int)pg_elem(dtype), n = 16 / size;
+  bool vec = a.rot.n_pairs % n == 0;
+  a.tail = 0;
+  a.n_heads[1] = 0;
+  for (int i = 0; i < (k ? 2 : 1); ++i) {
+    const wnw_rows_t &in = i ? *k : *q, &out = i ? *k_out : *q_out;
+    if (in.n_heads < 1 || in.n_heads > 4096 || in.n_heads != out.n_heads) return WNW_ERR_INVALID_ARG;
+    if (n_tokens && (!in.dev || !out.dev || (uintptr_t)in.dev % size || (uintptr_t)out.dev % size)) return WNW_ERR_INVALID_ARG;
+    vec = vec && pg_vector_rows(in, dtype) && pg_vector_rows(out, dtype);
+    const bool same = in.dev == out.dev && in.row_stride == out.row_stride && in.head_stride == out.head_stride;
+    if (!same) a.tail = head_dim - 2 * a.rot.n_pairs;
+    a.in[i] = rows_view(in);
+    a.out[i] = rows_view(out);
+    a.n_heads[i] = in.n_heads;
+  }
+  if (!n_tokens) return WNW_OK;
+  if (!positions_dev || (uintptr_t)positions_dev % 4) return WNW_ERR_INVALID_ARG;
+  a.positions = positions_dev;
+  a.axis_stride = axis_stride;
+  a.n_tokens = n_tokens;
+  a.head_dim = head_dim;
+  OnDevice on(device);
+  int n_sm = 0;
+  if (!on.ok || pg_sms(device, &n_sm) != WNW_OK) return WNW_ERR_CUDA;
+  a.tokens_per_cta = std::max(1, std::min(16, n_tokens / (n_sm * 8)));
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const cudaError_t e = dtype == WNW_DTYPE_BF16 ? launch<__nv_bfloat16>(a, vec, st) : dtype == WNW_DTYPE_FP16 ? launch<__half>(a, vec, st)
+                                                                                                              : launch<float>(a, vec, st);
+  return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
+}
