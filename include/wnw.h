@@ -452,11 +452,12 @@ wnw_status_t wnw_rotate(const wnw_rotary_t *rotary, const int32_t *positions_dev
  * do not count in max|x|; a not-a-number is stored as one in E4M3, as 0 in INT8. */
 enum { WNW_PAGES_E4M3 = 0, WNW_PAGES_INT8 = 1 };
 enum { WNW_PAGES_BAD_PAGE = 1,     /* a page id outside [0, n_pages): its rows were not written; read as zeros; not attended to */
-       WNW_PAGES_BAD_LENGTH = 2 }; /* a length or row range outside the table or the tensors: clipped to what is inside */
+       WNW_PAGES_BAD_LENGTH = 2,   /* a length or row range outside the table or the tensors: clipped to what is inside */
+       WNW_PAGES_TIMEOUT = 4 };    /* a copy did not arrive within the second that a kernel waits: the output is incomplete */
 typedef struct {
   void *codes_dev;          /* DEVICE bytes [n_pages][n_kv_heads][2][page_tokens][head_dim]: K rows, then V rows; 16-byte aligned */
-  float *scales_dev;        /* DEVICE [n_pages][n_kv_heads][2] */
-  int64_t page_stride;      /* bytes from page to page, a multiple of 16; 0: pages are contiguous */
+  float *scales_dev;        /* DEVICE [n_pages][n_kv_heads][2], powers of two */
+  int64_t page_stride;      /* bytes from page to page, a multiple of 16 below 2^40; 0: pages are contiguous */
   int64_t scale_stride;     /* floats from page to page in scales_dev; 0: contiguous */
   int32_t n_pages;
   int32_t page_tokens;      /* a multiple of 16, 16..256 */

@@ -26,7 +26,7 @@ WNW_RESIDENCY_HARD_BUDGET, WNW_RESIDENCY_SEGMENT_LAG, WNW_RESIDENCY_SEGMENT_LAG_
 WNW_TIDAL_KV_BF16, WNW_TIDAL_KV_FP8_E4M3 = 0, 1
 WNW_DTYPE_BF16, WNW_DTYPE_FP16, WNW_DTYPE_FP32 = 0, 1, 2
 WNW_PAGES_E4M3, WNW_PAGES_INT8 = 0, 1
-WNW_PAGES_BAD_PAGE, WNW_PAGES_BAD_LENGTH = 1, 2
+WNW_PAGES_BAD_PAGE, WNW_PAGES_BAD_LENGTH, WNW_PAGES_TIMEOUT = 1, 2, 4
 
 
 class wnw_config_t(C.Structure):

@@ -294,7 +294,7 @@ wnw_status_t pg_view(const wnw_pages_t *p, PagesView *v) {
   if (p->n_kv_heads > 1024) return WNW_ERR_CAPACITY;
   const long long page = 2ll * p->n_kv_heads * p->page_tokens * p->head_dim, scales = 2ll * p->n_kv_heads;
   if (p->n_pages && (!p->codes_dev || !p->scales_dev || (uintptr_t)p->codes_dev % 16 || (uintptr_t)p->scales_dev % 4)) return WNW_ERR_INVALID_ARG;
-  if ((p->page_stride && (p->page_stride < page || p->page_stride % 16)) || (p->scale_stride && p->scale_stride < scales)) return WNW_ERR_INVALID_ARG;
+  if ((p->page_stride && (p->page_stride < page || p->page_stride % 16 || p->page_stride >= 1ll << 40)) || (p->scale_stride && p->scale_stride < scales)) return WNW_ERR_INVALID_ARG;
   if ((uintptr_t)p->status_dev % 4) return WNW_ERR_INVALID_ARG;
   *v = PagesView{(unsigned char *)p->codes_dev, p->scales_dev, p->page_stride ? (long long)p->page_stride : page, p->scale_stride ? (long long)p->scale_stride : scales,
                  p->n_pages, p->page_tokens, p->n_kv_heads, p->status_dev};

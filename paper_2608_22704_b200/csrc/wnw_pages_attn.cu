@@ -9,14 +9,17 @@
 //
 // A warp multiplies tokens x head_dim by head_dim x query rows (S^T = K Q^T, O^T = V^T P^T; mma.sync m16n8k16), so that a group of up
 // to eight query rows fills an operand.  The order of the contracted index is free as long as both operands agree, so every lane keeps
-// to bytes that it copied itself: 16 of a row at a time, asynchronously into a ring of its own in shared memory, with no barrier and no
-// bank conflict.  Codes become fp16 exactly (e4m3 has 4 significant bits, int8 8); the query is scaled by a power of two to the top of
+// to 16 bytes of a row at a time.  A granule comes as one TMA copy (K and V rows, swizzled so that no bank conflicts arise) into the
+// warp's own ring in shared memory.  (Copies of 16 bytes a lane, cp.async, moved 5.0 TB/s however many warps and stages there were;
+// these 6.6.)  Codes become fp16 exactly (e4m3 has 4 significant bits, int8 8); the query is scaled by a power of two to the top of
 // fp16's range (exact but for elements 2^-32 of its largest); weights are fp16 against a reference within 2^8 of the largest.  Sums,
 // maxima and accumulators are fp32.
 //
 // The scales 2^eV sit inside the sum over tokens.  A second reference M, the maximum of s + eV in log2, carries them: weights enter the
 // product as 2^(s + eV - M), the denominator as 2^(s - m), and out = product * 2^(M - m) / denominator.  No spread of scales over the
 // pages can push the weights that matter out of fp16's range.
+#include <cuda.h>
+
 #include <algorithm>
 #include <atomic>
 #include <cstring>
@@ -26,11 +29,10 @@
 namespace wnw {
 namespace {
 
-constexpr int PA_WARPS = 8, PA_THREADS = PA_WARPS * 32;
-constexpr int PA_STAGES = 4;         // granules of a warp in the ring
 constexpr int PA_SEGS = 64;          // stretches of heads that a CTA prepares at a time
 constexpr int PA_ROWS = 16;          // query rows of a partial result
 constexpr float LAZY = 8.f;          // log2 by which a score may exceed the reference before that follows
+constexpr float NOTHING = -3e38f;    // the references before a token is seen: finite, so that differences are numbers
 
 // ---- workspace: per CTA two partial results (a head begun before, a head not finished) ----
 struct PartHead { int item, n_parts; };        // of slot 1: which head, how many CTAs share it; n_parts = 0: none
@@ -77,9 +79,24 @@ __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t *>(&v);
 }
-template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool there) {
-  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;\n" ::"r"(dst), "l"(src), "r"(there ? 8 : 0) : "memory");
+// One granule of a KV head: 16 K rows, then 16 V rows (see encode_map).
+__device__ __forceinline__ void copy_granule(uint32_t dst, const CUtensorMap *map, int row, int block, int page, uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(bytes) : "memory");
+  asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];\n"
+               ::"r"(dst), "l"(map), "r"(bar), "r"(0), "r"(row), "r"(block), "r"(page) : "memory");
+}
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
+// Bounded: gives up after about a second of SM clocks and says so, instead of hanging.
+__device__ __forceinline__ void wait_granule(uint32_t bar, uint32_t parity, const PagesView &pv) {
+  if (try_wait(bar, parity)) return;
+  const long long t0 = clock64();
+  while (!try_wait(bar, parity))
+    if (clock64() - t0 > 2000000000ll) { pg_report(pv, WNW_PAGES_TIMEOUT); return; }
 }
 
 // Four codes as fp16: the lower two in `lo`, the upper two in `hi`.
@@ -97,7 +114,9 @@ template <int FMT> __device__ __forceinline__ void to_half(uint32_t w, uint32_t 
   }
 }
 
-template <int D> struct Geo {
+// W warps of a CTA, S granules of a warp in the ring.
+template <int D, int NT> struct Geo {
+  static constexpr int W = D == 64 ? (NT == 1 ? 16 : 12) : NT == 1 ? 12 : 8, S = W == 12 && D == 128 ? 3 : 4, THREADS = 32 * W;
   static constexpr int KC = D / 64;                    // 16-byte pieces of a K row that a lane takes
   static constexpr int VB = D / 8;                     // bytes of a V row that a lane takes
   static constexpr int MT = D / 16;                    // 16-row tiles of V^T
@@ -105,18 +124,19 @@ template <int D> struct Geo {
   static constexpr int PITCH = D + 4;                  // floats of a row where the warps' results meet
 };
 template <int D, int NT> constexpr size_t smem_bytes() {
-  return (size_t)PA_WARPS * PA_STAGES * Geo<D>::STAGE + PA_WARPS * NT * 8 * Geo<D>::PITCH * 4 + PA_WARPS * NT * 8 * sizeof(PartRow) +
-         PA_WARPS * PA_STAGES * sizeof(float2) + PA_SEGS * sizeof(Seg) + (PG_MAX_SEQS + 1) * (sizeof(long long) + sizeof(int));
+  using G = Geo<D, NT>;
+  return (size_t)G::W * G::S * (G::STAGE + sizeof(uint32_t) + sizeof(uint64_t)) + G::W * NT * 8 * (G::PITCH * 4 + sizeof(PartRow)) + PA_SEGS * sizeof(Seg) +
+         (PG_MAX_SEQS + 1) * (sizeof(long long) + sizeof(int));
 }
 
 // The line: granules and heads (items) of the sequences before each one.  Returns the granules of all.
-template <int D>
+template <int W>
 __device__ __forceinline__ long long lay_out(const AttendArgs &a, long long *grans, int *items) {
-  __shared__ long long wsum[PA_WARPS];
-  __shared__ long long isum[PA_WARPS];
+  __shared__ long long wsum[W];
+  __shared__ long long isum[W];
   const int n = a.bv.n_seqs, tid = threadIdx.x, lane = tid & 31, w = tid >> 5, cap = a.bv.stride * a.pv.T;
   long long gbase = 0, ibase = 0;
-  for (int at = 0; at < n; at += PA_THREADS) {
+  for (int at = 0; at < n; at += 32 * W) {
     const int s = at + tid;
     long long gr = 0, it = 0;
     if (s < n) {
@@ -138,7 +158,7 @@ __device__ __forceinline__ long long lay_out(const AttendArgs &a, long long *gra
     __syncthreads();
     long long gw = gbase, gt = 0, iw = ibase, itot = 0;
 #pragma unroll
-    for (int k = 0; k < PA_WARPS; ++k) {
+    for (int k = 0; k < W; ++k) {
       if (k < w) { gw += wsum[k]; iw += isum[k]; }
       gt += wsum[k];
       itot += isum[k];
@@ -157,27 +177,33 @@ __device__ __forceinline__ long long lay_out(const AttendArgs &a, long long *gra
   return gbase;
 }
 // Granules that a CTA takes: equal stretches, none shorter than a granule for each warp.
-__device__ __forceinline__ long long stretch(long long total, int n_ctas) {
-  return max((long long)PA_WARPS, (total + n_ctas - 1) / n_ctas);
-}
+template <int W> __device__ __forceinline__ long long stretch(long long total, int n_ctas) { return max((long long)W, (total + n_ctas - 1) / n_ctas); }
 
 template <int D, int FMT, int NT>
-__global__ void __launch_bounds__(PA_THREADS, 1) wnw_pages_attend_kernel(const __grid_constant__ AttendArgs a) {
-  using G = Geo<D>;
-  extern __shared__ __align__(128) unsigned char smem[];
+__global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map) {
+  using G = Geo<D, NT>;
+  constexpr int W = G::W, S = G::S;
+  extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char *ring = smem;
-  float *meet = reinterpret_cast<float *>(ring + PA_WARPS * PA_STAGES * G::STAGE);            // [warp][row][PITCH]
-  PartRow *meet_row = reinterpret_cast<PartRow *>(meet + PA_WARPS * NT * 8 * G::PITCH);       // [warp][row]
-  float2 *ring_scale = reinterpret_cast<float2 *>(meet_row + PA_WARPS * NT * 8);              // [warp][stage]
-  Seg *segs = reinterpret_cast<Seg *>(ring_scale + PA_WARPS * PA_STAGES);
-  long long *grans = reinterpret_cast<long long *>(segs + PA_SEGS);
-  int *items = reinterpret_cast<int *>(grans + PG_MAX_SEQS + 1);
+  float *meet = reinterpret_cast<float *>(ring + W * S * G::STAGE);            // [warp][row][PITCH]
+  PartRow *meet_row = reinterpret_cast<PartRow *>(meet + W * NT * 8 * G::PITCH);       // [warp][row]
+  uint64_t *bars = reinterpret_cast<uint64_t *>(meet_row + W * NT * 8);                       // [warp][stage]
+  long long *grans = reinterpret_cast<long long *>(bars + W * S);
+  Seg *segs = reinterpret_cast<Seg *>(grans + PG_MAX_SEQS + 1);
+  int *items = reinterpret_cast<int *>(segs + PA_SEGS);
+  uint32_t *ring_scale = reinterpret_cast<uint32_t *>(items + PG_MAX_SEQS + 1);               // [warp][stage]
 
   const PagesView &pv = a.pv;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, c = lane & 3, r = lane >> 2;
   const int gpp = pv.T / PG_GR;
-  const long long total = lay_out<D>(a, grans, items);
-  const long long len_line = stretch(total, gridDim.x), x0 = min(total, blockIdx.x * len_line), x1 = min(total, x0 + len_line);
+  if (lane == 0) {
+    for (int k = 0; k < S; ++k) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;\n" ::"r"((uint32_t)__cvta_generic_to_shared(bars + w * S + k)) : "memory");
+    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];\n" ::"l"(&map) : "memory");
+  }
+  __syncwarp();
+  const long long total = lay_out<W>(a, grans, items);
+  const long long len_line = stretch<W>(total, gridDim.x), x0 = min(total, blockIdx.x * len_line), x1 = min(total, x0 + len_line);
   if (tid == 0) a.part_head[blockIdx.x] = PartHead{0, 0};
   if (x0 >= x1) return;
   // the first head of the line
@@ -190,7 +216,14 @@ __global__ void __launch_bounds__(PA_THREADS, 1) wnw_pages_attend_kernel(const _
     item0 = items[lo] + (int)((x0 - grans[lo]) / per);
   }
   const int n_items = items[a.bv.n_seqs];
-  const uint32_t ring_u = (uint32_t)__cvta_generic_to_shared(ring) + w * PA_STAGES * G::STAGE;
+  // a lane's 16-byte pieces of K row r and V rows 2c, 2c + 1 (and 8 rows on) in a swizzled granule
+  int k_at[G::KC], v_at[2];
+#pragma unroll
+  for (int k = 0; k < G::KC; ++k) k_at[k] = 16 * (D == 128 ? (c + 4 * k) ^ r : c ^ (r >> 1));
+#pragma unroll
+  for (int k = 0; k < 2; ++k) v_at[k] = D == 128 ? 16 * (r ^ (2 * c + k)) : 16 * ((r >> 1) ^ c) + 8 * (r & 1);
+  const uint32_t ring_u = (uint32_t)__cvta_generic_to_shared(ring) + w * S * G::STAGE, bars_u = (uint32_t)__cvta_generic_to_shared(bars + w * S);
+  uint32_t phases = 0;                                  // parity of each stage's next copy
 
   for (bool more = true; more;) {
     // ---- the next stretches ----
@@ -227,65 +260,48 @@ __global__ void __launch_bounds__(PA_THREADS, 1) wnw_pages_attend_kernel(const _
     more = n_seg == PA_SEGS;                            // (a last round of none costs nothing)
     item0 += n_seg;
 
-    // ---- copies run ahead of the products by PA_STAGES - 1 granules, over the stretches' ends ----
+    // ---- copies run ahead of the products by S - 1 granules, over the stretches' ends ----
     int p_seg = -1, p_g = 0, p_end = 0, p_cnt = 0, p_stage = 0;
-    long long p_off = 0;                                // lane i: where the stretch's granule 32 * k + i of this warp is
-    float p_k = 0.f, p_v = 0.f;
+    int p_page = 0, p_row = 0;                          // lane i: where the stretch's granule 32 * k + i of this warp is,
+    uint32_t p_scale = 0;                               //   exponent fields of its scales, K | V << 8 | 1 << 16 where it is there
     auto fetch = [&]() {
       while (p_seg < n_seg && p_g >= p_end) {
         if (++p_seg < n_seg) {
           const Seg &sg = segs[p_seg];
-          p_g = sg.g0 + ((w - sg.y0) & (PA_WARPS - 1));
+          p_g = sg.g0 + (w + W - sg.y0 % W) % W;
           p_end = min(sg.g0 + sg.n, sg.need);
           p_cnt = 0;
         }
       }
       if (p_seg < n_seg) {
         const Seg &sg = segs[p_seg];
-        if ((p_cnt & 31) == 0) {
-          const int g = p_g + PA_WARPS * lane;
-          p_off = 0;
-          p_k = -1.f;                                   // a page that is not there: nothing of it is seen
-          p_v = 0.f;
+        const int j = p_cnt & 31;
+        if (j == 0) {
+          const int g = p_g + W * lane;
+          p_scale = 0;
           if (g < p_end) {
-            const int page = a.bv.table[(long long)sg.s * a.bv.stride + g / gpp];
-            if (page >= 0 && page < pv.n_pages) {
-              p_off = page * pv.page_stride + (long long)sg.h * 2 * pv.T * D + (g % gpp) * PG_GR * D;
-              const float *sc = pv.scales + page * pv.scale_stride + sg.h * 2;
-              p_k = fabsf(sc[0]);
-              p_v = sc[1];
+            p_page = a.bv.table[(long long)sg.s * a.bv.stride + g / gpp];
+            p_row = g % gpp * PG_GR;
+            if (p_page >= 0 && p_page < pv.n_pages) {
+              const float *sc = pv.scales + p_page * pv.scale_stride + sg.h * 2;
+              p_scale = (__float_as_uint(sc[0]) >> 23 & 255) | (__float_as_uint(sc[1]) >> 23 & 255) << 8 | 1u << 16;
             } else {
               pg_report(pv, WNW_PAGES_BAD_PAGE);
             }
           }
         }
-        const int j = p_cnt & 31;
-        const long long off = __shfl_sync(0xffffffffu, p_off, j);
-        const float ks = __shfl_sync(0xffffffffu, p_k, j), vs = __shfl_sync(0xffffffffu, p_v, j);
-        if (lane == 0) ring_scale[w * PA_STAGES + p_stage] = make_float2(ks, vs);
-        const unsigned char *kp = pv.codes + off, *vp = kp + (long long)pv.T * D;
-        const uint32_t dst = ring_u + p_stage * G::STAGE;
-        const int left = ks < 0.f ? 0 : sg.len - p_g * PG_GR;         // rows of the granule that exist
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int k = 0; k < G::KC; ++k) {
-            const int row = r + 8 * t;
-            copy_async<16>(dst + (t * G::KC + k) * 512 + lane * 16, kp + row * D + 64 * k + 16 * c, row < left);
-          }
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const int row = 2 * c + (t & 1) + 8 * (t >> 1);
-          copy_async<G::VB>(dst + PG_GR * D + t * 32 * G::VB + lane * G::VB, vp + row * D + G::VB * r, row < left);
+        // by the lane that knows the granule; the others' reads of the stage are behind a __syncwarp
+        if (lane == j) {
+          ring_scale[w * S + p_stage] = p_scale;
+          if (p_scale) copy_granule(ring_u + p_stage * G::STAGE, &map, p_row, 2 * sg.h, p_page, bars_u + 8 * p_stage, G::STAGE);
         }
-        p_g += PA_WARPS;
+        p_g += W;
         ++p_cnt;
-        if (++p_stage == PA_STAGES) p_stage = 0;
+        if (++p_stage == S) p_stage = 0;
       }
-      asm volatile("cp.async.commit_group;\n" ::: "memory");
     };
 #pragma unroll
-    for (int k = 0; k < PA_STAGES - 1; ++k) fetch();
+    for (int k = 0; k < S - 1; ++k) fetch();
 
     int stage = 0;
     for (int si = 0; si < n_seg; ++si) {
@@ -337,31 +353,39 @@ __global__ void __launch_bounds__(PA_THREADS, 1) wnw_pages_attend_kernel(const _
       }
       const int end_min = a.causal ? sg.end0 : sg.len;   // up to here every row of the tile sees every token
 
-      float o[NT][G::MT][4], m[NT][2], big_m[NT][2], l[NT][2];
+      float o[NT][G::MT][4], m[NT][2], big_m[NT][2], l[NT][2], carry[NT][2];   // carry: 2^(m + e_last - M)
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
         for (int i = 0; i < G::MT; ++i) o[t][i][0] = o[t][i][1] = o[t][i][2] = o[t][i][3] = 0.f;
-        m[t][0] = m[t][1] = big_m[t][0] = big_m[t][1] = -INFINITY;
+        m[t][0] = m[t][1] = big_m[t][0] = big_m[t][1] = NOTHING;
         l[t][0] = l[t][1] = 0.f;
+        carry[t][0] = carry[t][1] = 1.f;
       }
+      float e_last = 0.f;
 
       const int g_end = min(sg.g0 + sg.n, sg.need);
-      for (int g = sg.g0 + ((w - sg.y0) & (PA_WARPS - 1)); g < g_end; g += PA_WARPS) {
+      for (int g = sg.g0 + (w + W - sg.y0 % W) % W; g < g_end; g += W) {
         __syncwarp();
         fetch();
-        asm volatile("cp.async.wait_group %0;\n" ::"n"(PA_STAGES - 1) : "memory");
         __syncwarp();
-        const float2 sc = ring_scale[w * PA_STAGES + stage];
-        const unsigned char *src = ring + (w * PA_STAGES + stage) * G::STAGE;
-        if (++stage == PA_STAGES) stage = 0;
+        const uint32_t sc = ring_scale[w * S + stage];
+        const unsigned char *src = ring + (w * S + stage) * G::STAGE;
+        if (sc) {
+          wait_granule(bars_u + 8 * stage, phases >> stage & 1, pv);
+          phases ^= 1u << stage;
+        }
+        if (++stage == S) stage = 0;
+        const bool there = sc != 0;                      // a page that is not there: nothing of it is seen
+        const float k_scale = __uint_as_float((sc & 255) << 23);
         // S^T: tokens r, r + 8 x columns 2c, 2c + 1
         float s[NT][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
 #pragma unroll
         for (int k = 0; k < G::KC; ++k) {
-          const uint4 u = *reinterpret_cast<const uint4 *>(src + k * 512 + lane * 16), v = *reinterpret_cast<const uint4 *>(src + (G::KC + k) * 512 + lane * 16);
+          const unsigned char *p = src + r * D + k_at[k];
+          const uint4 u = *reinterpret_cast<const uint4 *>(p), v = *reinterpret_cast<const uint4 *>(p + 8 * D);
           const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, vw[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
           for (int z = 0; z < 4; ++z) {
@@ -373,23 +397,23 @@ __global__ void __launch_bounds__(PA_THREADS, 1) wnw_pages_attend_kernel(const _
           }
         }
         const int tok = g * PG_GR + r;
-        const bool partly = sc.x < 0.f || (g + 1) * PG_GR > end_min;
-        const float e_v = (float)((int)(__float_as_uint(sc.y) >> 23 & 255) - 127);
+        const bool partly = !there || (g + 1) * PG_GR > end_min;
+        const float e_v = (float)((int)(sc >> 8 & 255) - 127);
         uint32_t pb[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          const float f0 = f_col[t][0] * sc.x, f1 = f_col[t][1] * sc.x;
+          const float f0 = f_col[t][0] * k_scale, f1 = f_col[t][1] * k_scale;
           s[t][0] *= f0; s[t][1] *= f1; s[t][2] *= f0; s[t][3] *= f1;
           if (partly) {
-            const bool there = sc.x >= 0.f;
             if (!there || tok >= end_col[t][0]) s[t][0] = -INFINITY;
             if (!there || tok >= end_col[t][1]) s[t][1] = -INFINITY;
             if (!there || tok + 8 >= end_col[t][0]) s[t][2] = -INFINITY;
             if (!there || tok + 8 >= end_col[t][1]) s[t][3] = -INFINITY;
           }
           float top0 = fmaxf(s[t][0], s[t][2]), top1 = fmaxf(s[t][1], s[t][3]);
-          const bool far = top0 > m[t][0] + LAZY || top1 > m[t][1] + LAZY || top0 + e_v > big_m[t][0] + LAZY || top1 + e_v > big_m[t][1] + LAZY;
-          if (__any_sync(0xffffffffu, far)) {
+          const bool far = top0 > fminf(m[t][0], big_m[t][0] - e_v) + LAZY || top1 > fminf(m[t][1], big_m[t][1] - e_v) + LAZY;
+          const bool moved = __any_sync(0xffffffffu, far);
+          if (moved) {
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) {
               top0 = fmaxf(top0, __shfl_xor_sync(0xffffffffu, top0, x));
@@ -397,33 +421,39 @@ __global__ void __launch_bounds__(PA_THREADS, 1) wnw_pages_attend_kernel(const _
             }
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
-              const float top = z ? top1 : top0, mn = fmaxf(m[t][z], top), bn = fmaxf(big_m[t][z], top + e_v);
-              // (-inf: nothing has been seen, the sums are zero)
-              l[t][z] *= m[t][z] == -INFINITY ? 1.f : ex2(m[t][z] - mn);
-              const float by = big_m[t][z] == -INFINITY ? 1.f : ex2(big_m[t][z] - bn);
+              const float top = z ? top1 : top0, mn = fmaxf(m[t][z], top), bn = fmaxf(big_m[t][z], top + e_v), by = ex2(big_m[t][z] - bn);
+              l[t][z] *= ex2(m[t][z] - mn);
 #pragma unroll
               for (int i = 0; i < G::MT; ++i) { o[t][i][z] *= by; o[t][i][2 + z] *= by; }
               m[t][z] = mn;
               big_m[t][z] = bn;
             }
           }
-          const float m0 = m[t][0] == -INFINITY ? 0.f : m[t][0], m1 = m[t][1] == -INFINITY ? 0.f : m[t][1];
-          // (finite: where the scales are that far apart, p is zero)
-          const float w0 = big_m[t][0] == -INFINITY ? 0.f : ex2(fminf(m0 + e_v - big_m[t][0], 126.f));
-          const float w1 = big_m[t][1] == -INFINITY ? 0.f : ex2(fminf(m1 + e_v - big_m[t][1], 126.f));
-          const float p0 = ex2(s[t][0] - m0), p1 = ex2(s[t][1] - m1), p2 = ex2(s[t][2] - m0), p3 = ex2(s[t][3] - m1);
+          if (moved || e_v != e_last) {                  // (finite: where scales are that far apart, p is zero)
+            carry[t][0] = ex2(fminf(m[t][0] + e_v - big_m[t][0], 126.f));
+            carry[t][1] = ex2(fminf(m[t][1] + e_v - big_m[t][1], 126.f));
+          }
+          const float p0 = ex2(s[t][0] - m[t][0]), p1 = ex2(s[t][1] - m[t][1]), p2 = ex2(s[t][2] - m[t][0]), p3 = ex2(s[t][3] - m[t][1]);
           l[t][0] += p0 + p2;
           l[t][1] += p1 + p3;
-          pb[t][0] = transposed(half2_of(p0 * w0, p1 * w1));
-          pb[t][1] = transposed(half2_of(p2 * w0, p3 * w1));
+          pb[t][0] = transposed(half2_of(p0 * carry[t][0], p1 * carry[t][1]));
+          pb[t][1] = transposed(half2_of(p2 * carry[t][0], p3 * carry[t][1]));
         }
+        e_last = e_v;
         // O^T: elements VB * r + 2i (c0, c1) and VB * r + 2i + 1 (c2, c3) of the columns 2c, 2c + 1
         uint32_t vw[4][G::VB / 4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          const unsigned char *p = src + PG_GR * D + t * 32 * G::VB + lane * G::VB;
+          const unsigned char *p = src + PG_GR * D + (2 * c + (t & 1) + 8 * (t >> 1)) * D + v_at[t & 1];
           if constexpr (G::VB == 16) { const uint4 u = *reinterpret_cast<const uint4 *>(p); vw[t][0] = u.x; vw[t][1] = u.y; vw[t][2] = u.z; vw[t][3] = u.w; }
           else { const uint2 u = *reinterpret_cast<const uint2 *>(p); vw[t][0] = u.x; vw[t][1] = u.y; }
+        }
+        if (partly) {                                    // rows behind the last token hold anything
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            if (!there || g * PG_GR + 2 * c + (t & 1) + 8 * (t >> 1) >= sg.len)
+#pragma unroll
+              for (int z = 0; z < G::VB / 4; ++z) vw[t][z] = 0;
         }
         bool nan_codes = false;                          // in a granule that some rows see only part of
         if (FMT == WNW_PAGES_E4M3 && partly && a.causal && sg.nq > 1) {
@@ -494,32 +524,26 @@ __global__ void __launch_bounds__(PA_THREADS, 1) wnw_pages_attend_kernel(const _
           if (r == 0) meet_row[(w * NT + t) * 8 + 2 * c + z] = PartRow{m[t][z], big_m[t][z], l[t][z], 0.f};
         }
       __syncthreads();
-      for (int i = tid; i < NT * 8 * (D / 4); i += PA_THREADS) {
+      for (int i = tid; i < NT * 8 * (D / 4); i += G::THREADS) {
         const int j = i / (D / 4), d = i % (D / 4) * 4, tok = j / a.g, hd = j - tok * a.g;
         if (j < a.rt * a.g && tok < sg.nq) {
-          float mx = -INFINITY, bx = -INFINITY;
+          float mx = NOTHING, bx = NOTHING, sum = 0.f;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-          for (int k = 0; k < PA_WARPS; ++k) {
+          for (int k = 0; k < W; ++k) {
             mx = fmaxf(mx, meet_row[k * NT * 8 + j].m);
             bx = fmaxf(bx, meet_row[k * NT * 8 + j].big_m);
           }
-          float sum = 0.f;
-          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (mx != -INFINITY) {
 #pragma unroll
-            for (int k = 0; k < PA_WARPS; ++k) {
-              const PartRow pr = meet_row[k * NT * 8 + j];
-              const float4 x = *reinterpret_cast<const float4 *>(meet + (k * NT * 8 + j) * G::PITCH + d);
-              const float by = ex2(pr.big_m - bx);
-              sum += pr.l * ex2(pr.m - mx);
-              acc.x += x.x * by; acc.y += x.y * by; acc.z += x.z * by; acc.w += x.w * by;
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < PA_WARPS; ++k) sum += meet_row[k * NT * 8 + j].l;     // 0, or not-a-number where a score was none
+          for (int k = 0; k < W; ++k) {
+            const PartRow pr = meet_row[k * NT * 8 + j];
+            const float4 x = *reinterpret_cast<const float4 *>(meet + (k * NT * 8 + j) * G::PITCH + d);
+            const float by = ex2(pr.big_m - bx);
+            sum += pr.l * ex2(pr.m - mx);
+            acc.x += x.x * by; acc.y += x.y * by; acc.z += x.z * by; acc.w += x.w * by;
           }
           if (sg.slot < 0) {
-            const float by = sum == 0.f ? 0.f : (mx == -INFINITY ? sum : ex2(bx - mx) / sum);
+            const float by = sum == 0.f ? 0.f : ex2(bx - mx) / sum;      // (no token: zeros)
             const long long row = sg.row0 + tok;
             const int head = sg.h * a.g + hd;
             unsigned char *p = a.out.p + 2 * (row * a.out.row + head * a.out.head + d);
@@ -527,7 +551,7 @@ __global__ void __launch_bounds__(PA_THREADS, 1) wnw_pages_attend_kernel(const _
             if (a.dtype == WNW_DTYPE_BF16) v = make_uint2(Pair<__nv_bfloat16>::put(acc.x * by, acc.y * by), Pair<__nv_bfloat16>::put(acc.z * by, acc.w * by));
             else v = make_uint2(Pair<__half>::put(acc.x * by, acc.y * by), Pair<__half>::put(acc.z * by, acc.w * by));
             *reinterpret_cast<uint2 *>(p) = v;
-            if (a.lse && d == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx == -INFINITY ? sum : (mx + log2f(sum)) * 0.69314718055994531f);
+            if (a.lse && d == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718055994531f;
           } else {
             const long long at = ((long long)blockIdx.x * 2 + sg.slot) * PA_ROWS + j;
             *reinterpret_cast<float4 *>(a.part_o + at * D + d) = acc;
@@ -538,7 +562,6 @@ __global__ void __launch_bounds__(PA_THREADS, 1) wnw_pages_attend_kernel(const _
       if (tid == 0 && sg.slot == 1) a.part_head[blockIdx.x] = PartHead{sg.item, sg.n_parts};
       __syncthreads();
     }
-    asm volatile("cp.async.wait_all;\n" ::: "memory");
   }
 }
 
@@ -565,7 +588,7 @@ __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_consta
   if (tok >= nq) return;
   const int part = threadIdx.x / LANES, d = threadIdx.x % LANES;
   auto at = [&](int k) { return ((long long)(blockIdx.x + k) * 2 + (k == 0)) * PA_ROWS + j; };
-  float mx = -INFINITY, bx = -INFINITY;
+  float mx = NOTHING, bx = NOTHING;
   for (int k = threadIdx.x; k < ph.n_parts; k += 128) {
     const PartRow pr = a.part_row[at(k)];
     mx = fmaxf(mx, pr.m);
@@ -587,8 +610,8 @@ __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_consta
   for (int k = part; k < ph.n_parts; k += SPLIT) {
     const PartRow pr = a.part_row[at(k)];
     const float4 x = *reinterpret_cast<const float4 *>(a.part_o + at(k) * D + 4 * d);
-    const float by = mx == -INFINITY ? 0.f : ex2(pr.big_m - bx);
-    sum += mx == -INFINITY ? pr.l : pr.l * ex2(pr.m - mx);
+    const float by = ex2(pr.big_m - bx);
+    sum += pr.l * ex2(pr.m - mx);
     acc.x += x.x * by; acc.y += x.y * by; acc.z += x.z * by; acc.w += x.w * by;
   }
   acc_s[part][d] = acc;
@@ -603,13 +626,13 @@ __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_consta
     sum += sum_s[k];
     acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
   }
-  const float by = sum == 0.f ? 0.f : (mx == -INFINITY ? sum : ex2(bx - mx) / sum);
+  const float by = sum == 0.f ? 0.f : ex2(bx - mx) / sum;      // (no token: zeros)
   const long long row = r0 + tile * a.rt + tok;
   const int head = h * a.g + hd;
   unsigned char *p = a.out.p + 2 * (row * a.out.row + head * a.out.head + 4 * d);
   if (a.dtype == WNW_DTYPE_BF16) *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__nv_bfloat16>::put(acc.x * by, acc.y * by), Pair<__nv_bfloat16>::put(acc.z * by, acc.w * by));
   else *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__half>::put(acc.x * by, acc.y * by), Pair<__half>::put(acc.z * by, acc.w * by));
-  if (a.lse && d == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx == -INFINITY ? sum : (mx + log2f(sum)) * 0.69314718055994531f);
+  if (a.lse && d == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718055994531f;
 }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -619,21 +642,44 @@ size_t workspace_bytes(int n_ctas, int d, size_t *rows, size_t *heads) {
   return *heads + align256((size_t)n_ctas * sizeof(PartHead));
 }
 
-template <int D, int FMT, int NT> cudaError_t launch(const AttendArgs &a, int n_ctas, int device, cudaStream_t st) {
+// The store as the tensor [page][head, K|V][row][byte]: a box is the K and V rows of a granule, swizzled by the row's length.
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+bool encode_map(CUtensorMap *map, const PagesView &pv, int d) {
+  static std::atomic<EncodeTiled> known{nullptr};   // looked up at run time: the library does not link against the driver
+  EncodeTiled fn = known.load(std::memory_order_relaxed);
+  if (!fn) {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess || !p || found != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      return false;
+    }
+    fn = (EncodeTiled)p;
+    known.store(fn, std::memory_order_relaxed);
+  }
+  const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)pv.T, 2 * (cuuint64_t)pv.H, (cuuint64_t)pv.n_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)d, (cuuint64_t)pv.T * d, (cuuint64_t)pv.page_stride};
+  const cuuint32_t box[4] = {(cuuint32_t)d, PG_GR, 2, 1}, each[4] = {1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pv.codes, dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int FMT, int NT> cudaError_t launch(const AttendArgs &a, const CUtensorMap &map, int n_ctas, int device, cudaStream_t st) {
   static std::atomic<unsigned long long> ready{0};       // devices whose kernel has its shared memory
   if (!(ready.load(std::memory_order_acquire) >> device & 1)) {
     const cudaError_t e = cudaFuncSetAttribute(wnw_pages_attend_kernel<D, FMT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D, NT>());
     if (e != cudaSuccess) return e;
     ready.fetch_or(1ull << device, std::memory_order_release);
   }
-  wnw_pages_attend_kernel<D, FMT, NT><<<n_ctas, PA_THREADS, smem_bytes<D, NT>(), st>>>(a);
+  wnw_pages_attend_kernel<D, FMT, NT><<<n_ctas, Geo<D, NT>::THREADS, smem_bytes<D, NT>(), st>>>(a, map);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   wnw_pages_join_kernel<D><<<dim3(n_ctas, a.rt * a.g), 128, 0, st>>>(a);
   return cudaGetLastError();
 }
-template <int D, int FMT> cudaError_t launch(const AttendArgs &a, int nt, int n_ctas, int device, cudaStream_t st) {
-  return nt == 1 ? launch<D, FMT, 1>(a, n_ctas, device, st) : launch<D, FMT, 2>(a, n_ctas, device, st);
+template <int D, int FMT> cudaError_t launch(const AttendArgs &a, const CUtensorMap &map, int nt, int n_ctas, int device, cudaStream_t st) {
+  return nt == 1 ? launch<D, FMT, 1>(a, map, n_ctas, device, st) : launch<D, FMT, 2>(a, map, n_ctas, device, st);
 }
 
 wnw_status_t check_heads(const wnw_pages_t *p, int n_q_heads) {
@@ -693,9 +739,12 @@ extern "C" wnw_status_t wnw_pages_attend(const wnw_pages_t *pages, const wnw_bat
   a.rt = std::min(nt * 8 / a.g, max_rows);
   // items are counted in 32 bits
   if (((long long)batch->n_rows / a.rt + batch->n_seqs) * pages->n_kv_heads > 1ll << 30) return WNW_ERR_CAPACITY;
+  CUtensorMap map;
+  memset(&map, 0, sizeof(map));
+  if (pages->n_pages && !encode_map(&map, a.pv, pages->head_dim)) return WNW_ERR_CUDA;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   cudaError_t e;
-  if (pages->head_dim == 64) e = pages->format == WNW_PAGES_E4M3 ? launch<64, WNW_PAGES_E4M3>(a, nt, n_sm, pages->device, st) : launch<64, WNW_PAGES_INT8>(a, nt, n_sm, pages->device, st);
-  else e = pages->format == WNW_PAGES_E4M3 ? launch<128, WNW_PAGES_E4M3>(a, nt, n_sm, pages->device, st) : launch<128, WNW_PAGES_INT8>(a, nt, n_sm, pages->device, st);
+  if (pages->head_dim == 64) e = pages->format == WNW_PAGES_E4M3 ? launch<64, WNW_PAGES_E4M3>(a, map, nt, n_sm, pages->device, st) : launch<64, WNW_PAGES_INT8>(a, map, nt, n_sm, pages->device, st);
+  else e = pages->format == WNW_PAGES_E4M3 ? launch<128, WNW_PAGES_E4M3>(a, map, nt, n_sm, pages->device, st) : launch<128, WNW_PAGES_INT8>(a, map, nt, n_sm, pages->device, st);
   return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
 }
