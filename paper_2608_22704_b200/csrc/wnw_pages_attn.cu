@@ -24,32 +24,13 @@
 #include <atomic>
 #include <cstring>
 
-#include "wnw_pages.cuh"
+#include "wnw_pages_attn.cuh"
 
 namespace wnw {
 namespace {
 
+constexpr int PA_ROWS = 16;           // query rows of an item at most
 constexpr int PA_SEGS = 64;          // stretches of heads that a CTA prepares at a time
-constexpr int PA_ROWS = 16;          // query rows of a partial result
-constexpr float LAZY = 8.f;          // log2 by which a score may exceed the reference before that follows
-constexpr float NOTHING = -3e38f;    // the references before a token is seen: finite, so that differences are numbers
-
-// ---- workspace: per CTA two partial results (a head begun before, a head not finished) ----
-struct PartHead { int item, n_parts; };        // of slot 1: which head, how many CTAs share it; n_parts = 0: none
-struct PartRow { float m, big_m, l, pad; };
-
-struct AttendArgs {
-  PagesView pv;
-  BatchView bv;
-  RowsView q, out;
-  float *lse;
-  int Hq, g, rt;                     // query heads, group, query tokens of a tile
-  int dtype, causal;
-  float scale_log2;
-  float *part_o;                     // [CTA][2][PA_ROWS][D]
-  PartRow *part_row;                 // [CTA][2][PA_ROWS]
-  PartHead *part_head;               // [CTA]
-};
 
 // A head's stretch inside a CTA.
 struct Seg {
@@ -58,14 +39,9 @@ struct Seg {
   int need;                          // granules from the head's first on that some row sees
   int len, row0, nq;                 // tokens of the sequence; first query row and query tokens of the tile
   int end0;                          // tokens that the tile's first query row sees; the next rows see one more each if causal
-  int item, slot, n_parts;           // slot -1: the whole head; else where the partial result goes
+  int slot, n_parts;                 // slot -1: the whole head; else where the partial result goes
 };
 
-__device__ __forceinline__ float ex2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
-  return r;
-}
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -75,21 +51,11 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {   // an 8 x 8 matri
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(x));
   return r;
 }
-__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
-  const __half2 v = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
 // One granule of a KV head: 16 K rows, then 16 V rows (see encode_map).
 __device__ __forceinline__ void copy_granule(uint32_t dst, const CUtensorMap *map, int row, int block, int page, uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(bytes) : "memory");
   asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];\n"
                ::"r"(dst), "l"(map), "r"(bar), "r"(0), "r"(row), "r"(block), "r"(page) : "memory");
-}
-__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok;
 }
 // Bounded: gives up after about a second of SM clocks and says so, instead of hanging.
 __device__ __forceinline__ void wait_granule(uint32_t bar, uint32_t parity, const PagesView &pv) {
@@ -97,21 +63,6 @@ __device__ __forceinline__ void wait_granule(uint32_t bar, uint32_t parity, cons
   const long long t0 = clock64();
   while (!try_wait(bar, parity))
     if (clock64() - t0 > 2000000000ll) { pg_report(pv, WNW_PAGES_TIMEOUT); return; }
-}
-
-// Four codes as fp16: the lower two in `lo`, the upper two in `hi`.
-template <int FMT> __device__ __forceinline__ void to_half(uint32_t w, uint32_t &lo, uint32_t &hi) {
-  if constexpr (FMT == WNW_PAGES_E4M3) {
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(lo) : "h"((unsigned short)w));
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(hi) : "h"((unsigned short)(w >> 16)));
-  } else {   // code + 128 as the low byte of an fp16 number between 1024 and 2048, less 1152: exact
-    w ^= 0x80808080u;
-    const uint32_t x = __byte_perm(w, 0x64646464u, 0x4140), y = __byte_perm(w, 0x64646464u, 0x4342), off = 0x64806480u;
-    const __half2 o = *reinterpret_cast<const __half2 *>(&off);
-    const __half2 p = __hsub2(*reinterpret_cast<const __half2 *>(&x), o), q = __hsub2(*reinterpret_cast<const __half2 *>(&y), o);
-    lo = *reinterpret_cast<const uint32_t *>(&p);
-    hi = *reinterpret_cast<const uint32_t *>(&q);
-  }
 }
 
 // W warps of a CTA, S granules of a warp in the ring.
@@ -204,7 +155,7 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
   __syncwarp();
   const long long total = lay_out<W>(a, grans, items);
   const long long len_line = stretch<W>(total, gridDim.x), x0 = min(total, blockIdx.x * len_line), x1 = min(total, x0 + len_line);
-  if (tid == 0) a.part_head[blockIdx.x] = PartHead{0, 0};
+  if (tid == 0) a.part_head[blockIdx.x] = PartHead{0, 0, 0, 0};
   if (x0 >= x1) return;
   // the first head of the line
   int item0 = 0;
@@ -250,7 +201,6 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
           sg.end0 = a.causal ? sg.len - (r1 - r0) + sg.tile * a.rt + 1 : sg.len;
           const int last = min(sg.len, a.causal ? sg.end0 + sg.nq - 1 : sg.len);
           sg.need = last > 0 ? (last + PG_GR - 1) / PG_GR : 0;
-          sg.item = item;
           sg.slot = b >= x0 && e <= x1 ? -1 : b < x0 ? 0 : 1;
           sg.n_parts = (int)((e - 1) / len_line - b / len_line + 1);
         }
@@ -559,86 +509,81 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
           }
         }
       }
-      if (tid == 0 && sg.slot == 1) a.part_head[blockIdx.x] = PartHead{sg.item, sg.n_parts};
+      if (tid == 0 && sg.slot == 1) a.part_head[blockIdx.x] = PartHead{sg.s, sg.h, sg.tile, sg.n_parts};
       __syncthreads();
     }
   }
 }
 
-// A head that several CTAs share: CTA (b, j) puts row j of the head together that begins in CTA b of the attention and does not end there.
+// A head that several CTAs share: CTA (b, y) puts every gridDim.y-th row of the head together that begins in CTA b of the attention and
+// does not end there.
 template <int D>
 __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_constant__ AttendArgs a) {
   constexpr int LANES = D / 4, SPLIT = 128 / LANES;
   __shared__ float4 acc_s[SPLIT][LANES];
-  __shared__ float sum_s[SPLIT];
+  __shared__ float sum_s[SPLIT], red[2][4];
   const PartHead ph = a.part_head[blockIdx.x];
-  const int j = blockIdx.y, tok = j / a.g, hd = j - tok * a.g;
   if (ph.n_parts < 2) return;
-  // which rows: the item's sequence again
-  int s = 0, base = 0, tiles = 0, r0 = 0, r1 = 0;
-  for (; s < a.bv.n_seqs; ++s) {
-    r0 = max(a.bv.starts[s], 0);
-    r1 = min(a.bv.starts[s + 1], a.bv.n_rows);
-    tiles = r1 > r0 ? (r1 - r0 + a.rt - 1) / a.rt : 0;
-    if (ph.item < base + tiles * a.pv.H) break;
-    base += tiles * a.pv.H;
-  }
-  if (s == a.bv.n_seqs) return;
-  const int it = ph.item - base, h = it / tiles, tile = it % tiles, nq = min(a.rt, r1 - r0 - tile * a.rt);
-  if (tok >= nq) return;
+  const int r0 = max(a.bv.starts[ph.s], 0), n = min(a.bv.starts[ph.s + 1], a.bv.n_rows) - r0, used = a.rt * a.g;
   const int part = threadIdx.x / LANES, d = threadIdx.x % LANES;
-  auto at = [&](int k) { return ((long long)(blockIdx.x + k) * 2 + (k == 0)) * PA_ROWS + j; };
-  float mx = NOTHING, bx = NOTHING;
-  for (int k = threadIdx.x; k < ph.n_parts; k += 128) {
-    const PartRow pr = a.part_row[at(k)];
-    mx = fmaxf(mx, pr.m);
-    bx = fmaxf(bx, pr.big_m);
-  }
-  __shared__ float red[2][4];
+  for (int y = blockIdx.y; y < a.blocks * used; y += gridDim.y) {
+    const int i = y / used, jj = y - i * used, j = i * a.rb + jj, tok = (ph.tile * a.blocks + i) * a.rt + jj / a.g, hd = jj % a.g;
+    if (tok >= n) continue;
+    auto at = [&](int k) { return ((long long)(blockIdx.x + k) * 2 + (k == 0)) * (a.blocks * a.rb) + j; };
+    float mx = NOTHING, bx = NOTHING;
+    for (int k = threadIdx.x; k < ph.n_parts; k += 128) {
+      const PartRow pr = a.part_row[at(k)];
+      mx = fmaxf(mx, pr.m);
+      bx = fmaxf(bx, pr.big_m);
+    }
 #pragma unroll
-  for (int x = 16; x; x >>= 1) {
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
-    bx = fmaxf(bx, __shfl_xor_sync(0xffffffffu, bx, x));
-  }
-  if ((threadIdx.x & 31) == 0) { red[0][threadIdx.x >> 5] = mx; red[1][threadIdx.x >> 5] = bx; }
-  __syncthreads();
-  mx = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-  bx = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  float sum = 0.f;
+    for (int x = 16; x; x >>= 1) {
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+      bx = fmaxf(bx, __shfl_xor_sync(0xffffffffu, bx, x));
+    }
+    if ((threadIdx.x & 31) == 0) { red[0][threadIdx.x >> 5] = mx; red[1][threadIdx.x >> 5] = bx; }
+    __syncthreads();
+    mx = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    bx = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
 #pragma unroll 4
-  for (int k = part; k < ph.n_parts; k += SPLIT) {
-    const PartRow pr = a.part_row[at(k)];
-    const float4 x = *reinterpret_cast<const float4 *>(a.part_o + at(k) * D + 4 * d);
-    const float by = ex2(pr.big_m - bx);
-    sum += pr.l * ex2(pr.m - mx);
-    acc.x += x.x * by; acc.y += x.y * by; acc.z += x.z * by; acc.w += x.w * by;
-  }
-  acc_s[part][d] = acc;
-  if (d == 0) sum_s[part] = sum;
-  __syncthreads();
-  if (part) return;
-  sum = 0.f;
-  acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = part; k < ph.n_parts; k += SPLIT) {
+      const PartRow pr = a.part_row[at(k)];
+      const float4 x = *reinterpret_cast<const float4 *>(a.part_o + at(k) * D + 4 * d);
+      const float by = ex2(pr.big_m - bx);
+      sum += pr.l * ex2(pr.m - mx);
+      acc.x += x.x * by; acc.y += x.y * by; acc.z += x.z * by; acc.w += x.w * by;
+    }
+    acc_s[part][d] = acc;
+    if (d == 0) sum_s[part] = sum;
+    __syncthreads();
+    if (part == 0) {
+      sum = 0.f;
+      acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int k = 0; k < SPLIT; ++k) {
-    const float4 x = acc_s[k][d];
-    sum += sum_s[k];
-    acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+      for (int k = 0; k < SPLIT; ++k) {
+        const float4 x = acc_s[k][d];
+        sum += sum_s[k];
+        acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+      }
+      const float by = sum == 0.f ? 0.f : ex2(bx - mx) / sum;      // (no token: zeros)
+      const long long row = r0 + tok;
+      const int head = ph.h * a.g + hd;
+      unsigned char *p = a.out.p + 2 * (row * a.out.row + head * a.out.head + 4 * d);
+      if (a.dtype == WNW_DTYPE_BF16) *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__nv_bfloat16>::put(acc.x * by, acc.y * by), Pair<__nv_bfloat16>::put(acc.z * by, acc.w * by));
+      else *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__half>::put(acc.x * by, acc.y * by), Pair<__half>::put(acc.z * by, acc.w * by));
+      if (a.lse && d == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718055994531f;
+    }
+    __syncthreads();
   }
-  const float by = sum == 0.f ? 0.f : ex2(bx - mx) / sum;      // (no token: zeros)
-  const long long row = r0 + tile * a.rt + tok;
-  const int head = h * a.g + hd;
-  unsigned char *p = a.out.p + 2 * (row * a.out.row + head * a.out.head + 4 * d);
-  if (a.dtype == WNW_DTYPE_BF16) *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__nv_bfloat16>::put(acc.x * by, acc.y * by), Pair<__nv_bfloat16>::put(acc.z * by, acc.w * by));
-  else *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__half>::put(acc.x * by, acc.y * by), Pair<__half>::put(acc.z * by, acc.w * by));
-  if (a.lse && d == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718055994531f;
 }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+// part_o and part_row for the larger of the two forms, part_head
 size_t workspace_bytes(int n_ctas, int d, size_t *rows, size_t *heads) {
-  *rows = align256((size_t)n_ctas * 2 * PA_ROWS * d * sizeof(float));
-  *heads = *rows + align256((size_t)n_ctas * 2 * PA_ROWS * sizeof(PartRow));
+  *rows = align256((size_t)n_ctas * 2 * PP_BLOCKS * PP_ROWS * d * sizeof(float));
+  *heads = *rows + align256((size_t)n_ctas * 2 * PP_BLOCKS * PP_ROWS * sizeof(PartRow));
   return *heads + align256((size_t)n_ctas * sizeof(PartHead));
 }
 
@@ -673,9 +618,6 @@ template <int D, int FMT, int NT> cudaError_t launch(const AttendArgs &a, const 
     ready.fetch_or(1ull << device, std::memory_order_release);
   }
   wnw_pages_attend_kernel<D, FMT, NT><<<n_ctas, Geo<D, NT>::THREADS, smem_bytes<D, NT>(), st>>>(a, map);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
-  wnw_pages_join_kernel<D><<<dim3(n_ctas, a.rt * a.g), 128, 0, st>>>(a);
   return cudaGetLastError();
 }
 template <int D, int FMT> cudaError_t launch(const AttendArgs &a, const CUtensorMap &map, int nt, int n_ctas, int device, cudaStream_t st) {
@@ -734,17 +676,29 @@ extern "C" wnw_status_t wnw_pages_attend(const wnw_pages_t *pages, const wnw_bat
   a.part_o = (float *)workspace_dev;
   a.part_row = (PartRow *)((char *)workspace_dev + rows_at);
   a.part_head = (PartHead *)((char *)workspace_dev + heads_at);
-  const int max_rows = batch->max_rows > 0 ? std::min(batch->max_rows, batch->n_rows) : batch->n_rows;
+  const int max_rows = batch->max_rows > 0 ? std::min(batch->max_rows, batch->n_rows) : batch->n_rows, d = pages->head_dim;
+  const bool prompt = (long long)max_rows * a.g > 16;
   const int nt = (long long)max_rows * a.g <= 8 ? 1 : 2;
-  a.rt = std::min(nt * 8 / a.g, max_rows);
+  a.blocks = prompt ? PP_BLOCKS : 1;
+  a.rb = prompt ? PP_ROWS : PA_ROWS;
+  a.rt = prompt ? PP_ROWS / a.g : std::min(nt * 8 / a.g, max_rows);
   // items are counted in 32 bits
   if (((long long)batch->n_rows / a.rt + batch->n_seqs) * pages->n_kv_heads > 1ll << 30) return WNW_ERR_CAPACITY;
-  CUtensorMap map;
-  memset(&map, 0, sizeof(map));
-  if (pages->n_pages && !encode_map(&map, a.pv, pages->head_dim)) return WNW_ERR_CUDA;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   cudaError_t e;
-  if (pages->head_dim == 64) e = pages->format == WNW_PAGES_E4M3 ? launch<64, WNW_PAGES_E4M3>(a, map, nt, n_sm, pages->device, st) : launch<64, WNW_PAGES_INT8>(a, map, nt, n_sm, pages->device, st);
-  else e = pages->format == WNW_PAGES_E4M3 ? launch<128, WNW_PAGES_E4M3>(a, map, nt, n_sm, pages->device, st) : launch<128, WNW_PAGES_INT8>(a, map, nt, n_sm, pages->device, st);
+  if (prompt) {
+    e = launch_prompt(a, d, pages->format, n_sm, pages->device, st);
+  } else {
+    CUtensorMap map;
+    memset(&map, 0, sizeof(map));
+    if (pages->n_pages && !encode_map(&map, a.pv, d)) return WNW_ERR_CUDA;
+    if (d == 64) e = pages->format == WNW_PAGES_E4M3 ? launch<64, WNW_PAGES_E4M3>(a, map, nt, n_sm, pages->device, st) : launch<64, WNW_PAGES_INT8>(a, map, nt, n_sm, pages->device, st);
+    else e = pages->format == WNW_PAGES_E4M3 ? launch<128, WNW_PAGES_E4M3>(a, map, nt, n_sm, pages->device, st) : launch<128, WNW_PAGES_INT8>(a, map, nt, n_sm, pages->device, st);
+  }
+  if (e != cudaSuccess) return WNW_ERR_CUDA;
+  const dim3 grid(n_sm, prompt ? 16 : a.rt * a.g);
+  if (d == 64) wnw_pages_join_kernel<64><<<grid, 128, 0, st>>>(a);
+  else wnw_pages_join_kernel<128><<<grid, 128, 0, st>>>(a);
+  e = cudaGetLastError();
   return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
 }

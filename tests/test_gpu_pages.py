@@ -355,7 +355,7 @@ ROWS = [2, 3, 0, 20, 17, 4, 33]          # more rows than tokens: the first see 
 def test_attend_several_rows(fmt, hq, heads, d, T, causal):
     b = filled(fmt, heads, T, d, LENGTHS, seed=hq)
     q = randn(sum(ROWS) + 3, hq, d, seed=9, scale=2.0).to(DEV)
-    for max_rows in (0, 1, 4, 33):
+    for max_rows in (1, 4, 33, 0):
         out, lse = attend(b.pages, b.table_dev, LENGTHS, ROWS, q, causal=causal, max_rows=max_rows)
         check_attention(out, lse, q, values_of(b, LENGTHS), LENGTHS, ROWS, causal)
 
