@@ -34,7 +34,7 @@ struct Walk {
 };
 
 struct Shared {
-  uint64_t k_full[2], k_free[2], v_full[2], v_free[2], q_full[2], s_full[2], p_ready[2], o_done[2];
+  uint64_t k_full[2], k_free[2], v_full[2], v_free[2], q_full[2], s_full[2], p_ready[2], o_done[2], begun;
   uint32_t tmem;
   int dead;                          // a wait ran out: nobody waits any more
   uint32_t meta[4][8];               // per tile and granule: exponent fields of the scales, K | V << 8 | 1 << 16 where the page is there
@@ -250,6 +250,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
       for (uint64_t *b : {&sh.k_full[i], &sh.v_full[i], &sh.q_full[i], &sh.p_ready[i]}) asm volatile("mbarrier.init.shared::cta.b64 [%0], 4;\n" ::"r"(smem_u32(b)) : "memory");
       for (uint64_t *b : {&sh.k_free[i], &sh.v_free[i], &sh.s_full[i], &sh.o_done[i]}) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;\n" ::"r"(smem_u32(b)) : "memory");
     }
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;\n" ::"r"(smem_u32(&sh.begun)) : "memory");
     fence_smem();
     sh.dead = 0;
     a.part_head[blockIdx.x] = PartHead{0, 0, 0, 0};
@@ -273,13 +274,15 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
     const int i = wid >> 2, row = tid & 127, tok_in = row / a.g, hd = row - tok_in * a.g;
     const uint32_t lanes = (uint32_t)(wid & 3) << 21, t_s = tmem + lanes + COL_S + 128 * i, t_o = tmem + lanes + COL_O + 128 * i;
     uint32_t n_all = 0, n_mine = 0;                    // tiles of the CTA, and of this row tile, so far
-    int n_seg = 0;
+    int n_seg = 0, n_idle = 0;
     for (bool more = true; more; more = walk_on(a, w), ++n_seg) {
       const int n_tiles = w.k1 - w.k0;
-      if (i && !two_blocks(a, w)) {                    // (said all the same, so that a segment begins when the one before is out)
+      if (i && !two_blocks(a, w)) {
+        // Nothing to do; but a segment begins only when the one before it is out, and this warp is never two of them ahead.
         n_all += n_tiles;
         __syncwarp();
         if (lane == 0) arrive(&sh.q_full[1]);
+        wait(&sh.begun, n_idle++, sh, pv);
         continue;
       }
       const int first = (w.t * PP_BLOCKS + i) * a.rt, tok = first + tok_in;
@@ -628,6 +631,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
           fence_after();
           if (i == 0 || two) scores(i, n & 1);
         }
+        if (!two) arrive(&sh.begun);
         commit(&sh.k_free[n & 1]);
         for (int kt = w.k0; kt < w.k1; ++kt, ++n) {
           const int st = n & 1;

@@ -360,6 +360,18 @@ def test_attend_several_rows(fmt, hq, heads, d, T, causal):
         check_attention(out, lse, q, values_of(b, LENGTHS), LENGTHS, ROWS, causal)
 
 
+@pytest.mark.parametrize("fmt,heads,d,lengths,rows", [(E4M3, 8, 128, [4000], [130]), (INT8, 4, 64, [3000, 1, 2500], [70, 1, 200]), (E4M3, 4, 64, [1500, 1400, 0], [300, 65, 3]),
+                                                      (INT8, 6, 128, [2600], [65])])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attend_prompts(fmt, heads, d, lengths, rows, causal):
+    """Many tiles of tokens to a CTA, items of one and of two row tiles beside one another, items that several CTAs share."""
+    b = filled(fmt, heads, 64, d, lengths, seed=heads)
+    q = randn(sum(rows) + 1, 4 * heads, d, seed=9, scale=2.0).to(DEV)
+    out, lse = attend(b.pages, b.table_dev, lengths, rows, q, causal=causal)
+    check_attention(out, lse, q, values_of(b, lengths), lengths, rows, causal)
+    assert b.status.item() == 0
+
+
 @pytest.mark.parametrize("fmt,hq,heads,d", [(E4M3, 32, 8, 128), (INT8, 16, 2, 128), (E4M3, 8, 4, 64)])
 def test_attend_long_and_many(fmt, hq, heads, d):
     """One head spread over every CTA; and more heads than a CTA prepares at a time."""
