@@ -25,6 +25,9 @@ namespace {
 constexpr int PP_THREADS = 512, PP_TOKENS = 128;
 constexpr uint32_t COL_S = 0, COL_O = 256;
 
+constexpr uint32_t TILE_EVEN = 1;    // all granules have the same scales
+constexpr uint32_t TILE_HOLES = 2;   // a granule is not there, its page missing or the sequence at its end
+
 // Where a warp is on the line: the item and the tiles of it that fall to this CTA.  Every warp walks by itself.
 struct Walk {
   long long left;                    // tiles of the CTA's stretch from this segment on
@@ -37,8 +40,8 @@ struct Shared {
   uint64_t k_full[2], k_free[2], v_full[2], v_free[2], q_full[2], s_full[2], p_ready[2], o_done[2], begun;
   uint32_t tmem;
   int dead;                          // a wait ran out: nobody waits any more
-  uint32_t meta[4][8];               // per tile and granule: exponent fields of the scales, K | V << 8 | 1 << 16 where the page is there
-  uint32_t flags[4];                 // 1: all granules of the tile there, with the same scales
+  float2 scale[4][8];                // per tile and granule: 2^eK, eV; eV = -inf: the granule is not there
+  uint32_t flags[4];                 // TILE_* below
   // Not-a-numbers among the V codes, per warp that turns codes (each keeps its own), four segments deep (a slot is used again when the
   // slower row tile has left it): whether there are any, and then the first token that has one, per element.
   int nan_any[4][4], nan_first[4][4][128];
@@ -116,6 +119,95 @@ __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&x)[16
                "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]) : "memory");
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
+
+// ---- the softmax of a tile's 128 tokens, by the thread of a query row ----
+__device__ __forceinline__ uint64_t two(float x, float y) { return (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float lower(uint64_t x) { return __uint_as_float((uint32_t)x); }
+__device__ __forceinline__ float upper(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+
+// The largest score (`top`), and the largest with its V scale (`big`).  seen: of the tile's tokens, by the row.  32 tokens at a time, the
+// next ones on their way meanwhile; x[0] holds the first ones again afterwards.
+template <bool MASKED>
+__device__ __forceinline__ void row_top(uint32_t t_s, uint32_t (&x)[2][32], const float2 *scale, bool even, float f_row, int seen, float &top, float &big) {
+  top = -INFINITY;
+  big = NOTHING;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    tmem_loaded(x[k & 1]);
+    tmem_load(t_s + 32 * ((k + 1) & 3), x[(k + 1) & 1]);
+    float t[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      float y[16];
+#pragma unroll
+      for (int z = 0; z < 16; ++z) {
+        y[z] = __uint_as_float(x[k & 1][16 * g + z]);
+        if (MASKED && 32 * k + 16 * g + z >= seen) y[z] = -INFINITY;
+      }
+      t[g] = fmaxf(max3(max3(y[0], y[1], y[2]), max3(y[3], y[4], y[5]), max3(y[6], y[7], y[8])),
+                   max3(max3(y[9], y[10], y[11]), max3(y[12], y[13], y[14]), y[15]));
+    }
+    if (!MASKED && even) {
+      top = max3(top, t[0], t[1]);
+    } else {
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const float2 sc = scale[2 * k + g];
+        const float s = MASKED && (t[g] == -INFINITY || sc.y == -INFINITY) ? -INFINITY : t[g] * (f_row * sc.x);
+        top = fmaxf(top, s);
+        big = fmaxf(big, s + sc.y);
+      }
+    }
+  }
+  if (!MASKED && even) {
+    top *= f_row * scale[0].x;
+    big = top + scale[0].y;
+  }
+}
+// The weights 2^(s + eV - M), as fp16 to P's columns, and their sum as 2^(s - m) onto l.  They are taken as 2^(s - m - d), d = M - eV - m,
+// so that the sum is that of a granule times 2^d; where d is so large that weights that count in the denominator would vanish (a page of
+// zeros beside one of large values), d is 60 there and the rest a factor of its own (DEEP).  P's columns lie where S has been read.
+template <bool MASKED, bool DEEP>
+__device__ __forceinline__ void row_weights(uint32_t t_s, uint32_t (&x)[2][32], const float2 *scale, float f_row, int seen, float m, float big_m, float &l) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    tmem_loaded(x[k & 1]);
+    if (k < 3) tmem_load(t_s + 32 * (k + 1), x[(k + 1) & 1]);
+    uint32_t p[16];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const float2 sc = scale[2 * k + g];
+      const bool hole = MASKED && sc.y == -INFINITY;
+      const int lim = hole ? 0 : seen;
+      const float f = f_row * sc.x, d = hole ? 0.f : big_m - sc.y - m, d2 = DEEP ? fminf(d, 60.f) : d, off = -(m + d2), rest = DEEP ? ex2(d2 - d) : 1.f;
+      const uint64_t ff = two(f, f), oo = two(off, off);
+      uint64_t sum[2] = {0, 0};
+#pragma unroll
+      for (int z = 0; z < 16; z += 2) {
+        const uint64_t y = fma2(two(__uint_as_float(x[k & 1][16 * g + z]), __uint_as_float(x[k & 1][16 * g + z + 1])), ff, oo);
+        float u = ex2(lower(y)), v = ex2(upper(y));
+        if (MASKED && 32 * k + 16 * g + z >= lim) u = 0.f;
+        if (MASKED && 32 * k + 16 * g + z + 1 >= lim) v = 0.f;
+        sum[z >> 1 & 1] = add2(sum[z >> 1 & 1], two(u, v));
+        p[8 * g + z / 2] = DEEP ? half2_of(u * rest, v * rest) : half2_of(u, v);
+      }
+      const uint64_t both = add2(sum[0], sum[1]);
+      l = __fmaf_rn(lower(both) + upper(both), ex2(d2), l);
+    }
+    tmem_store(t_s + 16 * k, p);
+  }
+}
 
 // ---- the line ----
 // Query tokens, tokens and first row of a sequence, clipped to what is there; whether they had to be
@@ -327,45 +419,16 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
       for (int kt = w.k0; kt < w.k1; ++kt, ++n_all, ++n_mine) {
         wait(&sh.s_full[i], n_mine, sh, pv);
         fence_after();
-        // Two passes over the row, 32 tokens at a time, the next ones on their way meanwhile: the largest score, then the weights.  P's
-        // columns lie where S has been read already.
-        const uint32_t *meta = sh.meta[n_all & 3];
+        const float2 *scale = sh.scale[n_all & 3];
+        const uint32_t flags = sh.flags[n_all & 3];
         const int seen = end - kt * PP_TOKENS;         // of the tile's tokens
-        const bool plain = sh.flags[n_all & 3] && (kt + 1) * PP_TOKENS <= end_first;     // one pair of scales, every token seen
-        const float f_0 = f_row * __uint_as_float((meta[0] & 255) << 23), e_0 = (float)((int)(meta[0] >> 8 & 255) - 127);
+        const bool masked = (flags & TILE_HOLES) || (kt + 1) * PP_TOKENS > end_first;
         uint32_t x[2][32];
-        float top = -INFINITY, big = NOTHING;
-        bool far = false;
+        float top, big;
         tmem_load(t_s, x[0]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          tmem_loaded(x[k & 1]);
-          if (k < 3) tmem_load(t_s + 32 * (k + 1), x[(k + 1) & 1]);
-          if (plain) {
-#pragma unroll
-            for (int z = 0; z < 32; ++z) top = fmaxf(top, __uint_as_float(x[k & 1][z]));
-          } else {
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-              const uint32_t mt = meta[2 * k + g];
-              const float f = f_row * __uint_as_float((mt & 255) << 23), e = (float)((int)(mt >> 8 & 255) - 127);
-              const int here = mt ? seen - 32 * k - 16 * g : 0;
-              float t = -INFINITY;
-#pragma unroll
-              for (int z = 0; z < 16; ++z) t = fmaxf(t, z < here ? __uint_as_float(x[k & 1][16 * g + z]) * f : -INFINITY);
-              top = fmaxf(top, t);
-              big = fmaxf(big, t + e);
-              far = far || t > fminf(m, big_m - e) + LAZY;
-            }
-          }
-        }
-        tmem_load(t_s, x[0]);
-        if (plain) {
-          top *= f_0;
-          big = top + e_0;
-          far = top > fminf(m, big_m - e_0) + LAZY;
-        }
-        if (__any_sync(0xffffffffu, far)) {
+        if (masked) row_top<true>(t_s, x, scale, false, f_row, seen, top, big);
+        else row_top<false>(t_s, x, scale, flags & TILE_EVEN, f_row, seen, top, big);
+        if (__any_sync(0xffffffffu, top > m + LAZY || big > big_m + LAZY)) {
           const float mn = fmaxf(m, top), bn = fmaxf(big_m, big), by = ex2(big_m - bn);
           l *= ex2(m - mn);
           m = mn;
@@ -384,38 +447,16 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
             }
           }
         }
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        const float carry_0 = ex2(fminf(m + e_0 - big_m, 126.f));
+        bool deep = false;
+        if (!(flags & TILE_EVEN) || masked) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          tmem_loaded(x[k & 1]);
-          if (k < 3) tmem_load(t_s + 32 * (k + 1), x[(k + 1) & 1]);
-          uint32_t p[16];
-          if (plain) {
-#pragma unroll
-            for (int z = 0; z < 32; z += 2) {
-              const float u = ex2(__fmaf_rn(__uint_as_float(x[k & 1][z]), f_0, -m)), v = ex2(__fmaf_rn(__uint_as_float(x[k & 1][z + 1]), f_0, -m));
-              sum[z / 2 & 3] += u + v;
-              p[z / 2] = half2_of(u * carry_0, v * carry_0);
-            }
-          } else {
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-              const uint32_t mt = meta[2 * k + g];
-              const float f = f_row * __uint_as_float((mt & 255) << 23), carry = ex2(fminf(m + (float)((int)(mt >> 8 & 255) - 127) - big_m, 126.f));
-              const int here = mt ? seen - 32 * k - 16 * g : 0;
-#pragma unroll
-              for (int z = 0; z < 16; z += 2) {
-                const float u = z < here ? ex2(__fmaf_rn(__uint_as_float(x[k & 1][16 * g + z]), f, -m)) : 0.f;
-                const float v = z + 1 < here ? ex2(__fmaf_rn(__uint_as_float(x[k & 1][16 * g + z + 1]), f, -m)) : 0.f;
-                sum[z / 2 & 3] += u + v;
-                p[8 * g + z / 2] = half2_of(u * carry, v * carry);
-              }
-            }
-          }
-          tmem_store(t_s + 16 * k, p);
+          for (int g = 0; g < 8; ++g) deep = deep || (scale[g].y != -INFINITY && big_m - scale[g].y - m > 60.f);
+        } else {
+          deep = big_m - scale[0].y - m > 60.f;
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        if (__any_sync(0xffffffffu, deep)) row_weights<true, true>(t_s, x, scale, f_row, masked ? seen : PP_TOKENS, m, big_m, l);
+        else if (masked) row_weights<true, false>(t_s, x, scale, f_row, seen, m, big_m, l);
+        else row_weights<false, false>(t_s, x, scale, f_row, seen, m, big_m, l);
         tmem_stored();
         fence_before();
         __syncwarp();
@@ -540,11 +581,12 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
         const int st = n & 1;
         // scales: four tiles deep, so that the slower row tile's softmax has read them before they are overwritten
         const uint32_t meta = c.meta;
-        const uint32_t meta_0 = __shfl_sync(0xffffffffu, meta, 0), same = __ballot_sync(0xffffffffu, lane >= 8 || (meta && meta == meta_0));
+        const uint32_t meta_0 = __shfl_sync(0xffffffffu, meta, 0);
+        const bool even = __all_sync(0xffffffffu, lane >= 8 || meta == meta_0), holes = __any_sync(0xffffffffu, lane < 8 && !meta);
         wait(&sh.k_free[st], (n >> 1) + 1, sh, pv);
         if (wq == 0) {
-          if (lane < 8) sh.meta[n & 3][lane] = meta;
-          if (lane == 0) sh.flags[n & 3] = same == 0xffffffffu;
+          if (lane < 8) sh.scale[n & 3][lane] = make_float2(__uint_as_float((meta & 255) << 23), meta ? (float)((int)(meta >> 8 & 255) - 127) : -INFINITY);
+          if (lane == 0) sh.flags[n & 3] = (even ? TILE_EVEN : 0) | (holes ? TILE_HOLES : 0);
         }
         unsigned char *to = k_s + st * TILE + half * HALF;
         auto put = [&](unsigned char *tile, uint4 codes, int p) {
