@@ -395,7 +395,8 @@ wnw_status_t wnw_attend_static_status(int32_t device, void *cuda_stream, int32_t
 /* ---- Operators around a caller-owned, paged K/V store of eight bits -----------------------------------------------------
  * For callers that keep K,V themselves, as wnw_attend_static's do, but of many sequences, growing token by token, in pages,
  * and in a quarter of float's size.  None of the calls allocates, synchronises or keeps anything between calls; all queue
- * their work on cuda_stream and may be captured into a graph.  Every index that a kernel takes from device memory (page
+ * their work on cuda_stream and may be captured into a graph.  A call's arguments are one struct (HOST, read before the call
+ * returns).  Every index that a kernel takes from device memory (page
  * ids, lengths, row starts) is checked there before it is used: what lies outside is skipped, and if the caller gives a
  * status word, bits WNW_PAGES_* are set in it.  (The paper's footnote calls KV quantisation orthogonal to the method, and the
  * position encoding is the caller's job: the calls stand beside the cache, and wnw_pages_read hands its inputs over.) */
@@ -436,11 +437,21 @@ wnw_status_t wnw_rotary_init(wnw_rotary_t *rotary, int32_t n_pairs, double base,
  *                   bits, so far positions are as exact as near ones
  *   q, q_out      : n_tokens rows of heads of head_dim (2 to 256, even) elements of `dtype` (fp32 too); q_out may be q itself,
  *                   and must not overlap it otherwise
- *   k, k_out      : the same for the keys, or both NULL
+ *   k, k_out      : the same for the keys, or none (k.dev and k_out.dev NULL)
  * One rounding, at the end.  Strides and alignment are free here (16 bytes are faster). */
-wnw_status_t wnw_rotate(const wnw_rotary_t *rotary, const int32_t *positions_dev, int64_t axis_stride, int32_t n_tokens,
-                        int32_t head_dim, int32_t dtype, const wnw_rows_t *q, const wnw_rows_t *q_out, const wnw_rows_t *k,
-                        const wnw_rows_t *k_out, int32_t inverse, int32_t device, void *cuda_stream);
+typedef struct {
+  const wnw_rotary_t *rotary;
+  const int32_t *positions_dev;
+  int64_t axis_stride;
+  wnw_rows_t q, q_out, k, k_out;   /* k.dev = NULL: no keys */
+  int32_t n_tokens, head_dim;
+  int32_t dtype;                   /* WNW_DTYPE_* */
+  int32_t inverse;
+  int32_t device;                  /* CUDA ordinal of every pointer */
+  int32_t reserved;
+  void *cuda_stream;
+} wnw_rotate_t;
+wnw_status_t wnw_rotate(const wnw_rotate_t *call);
 
 /* The store.  A block = the rows of one page, one KV head, K or V; it has one scale 2^e, and a stored value is code * 2^e (an
  * exact bf16 number).
@@ -488,14 +499,22 @@ typedef struct {
  *   rotary, positions_dev : NULL, or turn the keys on the way (axes as in wnw_rotate, one position per row): the codes are those
  *                   of wnw_rotate's output.  2 * n_pairs <= head_dim, n_pairs a multiple of 8 (WNW_ERR_UNSUPPORTED)
  * A page that two sequences of a call write to holds a mixture afterwards; sequences share pages they only read. */
-wnw_status_t wnw_pages_write(const wnw_pages_t *pages, const wnw_batch_t *batch, const wnw_rows_t *k, const wnw_rows_t *v,
-                             int32_t dtype, const wnw_rotary_t *rotary, const int32_t *positions_dev, int64_t axis_stride,
-                             void *cuda_stream);
+typedef struct {
+  const wnw_pages_t *pages;
+  wnw_batch_t batch;
+  wnw_rows_t k, v;
+  const wnw_rotary_t *rotary;
+  const int32_t *positions_dev;
+  int64_t axis_stride;
+  int32_t dtype;
+  int32_t reserved;
+  void *cuda_stream;
+} wnw_pages_rows_t;
+wnw_status_t wnw_pages_write(const wnw_pages_rows_t *call);
 
 /* Reads tokens [lengths[s], lengths[s] + rows of s) of every sequence back into k and v (bf16 or fp16; a stored value beyond
  * fp16's largest becomes that). */
-wnw_status_t wnw_pages_read(const wnw_pages_t *pages, const wnw_batch_t *batch, const wnw_rows_t *k, const wnw_rows_t *v,
-                            int32_t dtype, void *cuda_stream);
+wnw_status_t wnw_pages_read(const wnw_pages_rows_t *call);   /* rotary must be NULL */
 
 /* Attention over the pages: out = softmax(q K^T * softmax_scale) V per query head, over tokens [0, lengths[s]) of the
  * sequence.  lengths counts the rows' own tokens: row i of n stands at token lengths[s] - n + i, and with causal = 1 sees the
@@ -506,9 +525,19 @@ wnw_status_t wnw_pages_read(const wnw_pages_t *pages, const wnw_batch_t *batch, 
  *   softmax_scale : 0 -> 1/sqrt(head_dim)
  *   workspace_dev : wnw_pages_attend_workspace bytes, 256-byte aligned; need not be initialised.  Calls that may overlap in time
  *                   (two streams, two graphs) need one each */
-wnw_status_t wnw_pages_attend(const wnw_pages_t *pages, const wnw_batch_t *batch, const wnw_rows_t *q, const wnw_rows_t *out,
-                              float *lse_dev, int32_t dtype, int32_t causal, float softmax_scale, void *workspace_dev,
-                              int64_t workspace_bytes, void *cuda_stream);
+typedef struct {
+  const wnw_pages_t *pages;
+  wnw_batch_t batch;
+  wnw_rows_t q, out;
+  float *lse_dev;
+  void *workspace_dev;
+  int64_t workspace_bytes;
+  int32_t dtype, causal;
+  float softmax_scale;
+  int32_t reserved;
+  void *cuda_stream;
+} wnw_pages_attend_t;
+wnw_status_t wnw_pages_attend(const wnw_pages_attend_t *call);
 wnw_status_t wnw_pages_attend_workspace(const wnw_pages_t *pages, int32_t n_q_heads, int64_t *bytes_host);
 
 const char *wnw_status_string(wnw_status_t status);

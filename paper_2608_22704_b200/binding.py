@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -63,6 +64,24 @@ class wnw_batch_t(C.Structure):
                 ("table_stride", C.c_int32), ("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("max_rows", C.c_int32)]
 
 
+class wnw_rotate_t(C.Structure):
+    _fields_ = [("rotary", C.c_void_p), ("positions_dev", C.c_void_p), ("axis_stride", C.c_int64), ("q", wnw_rows_t), ("q_out", wnw_rows_t),
+                ("k", wnw_rows_t), ("k_out", wnw_rows_t), ("n_tokens", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("inverse", C.c_int32), ("device", C.c_int32), ("reserved", C.c_int32), ("cuda_stream", C.c_void_p)]
+
+
+class wnw_pages_rows_t(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("batch", wnw_batch_t), ("k", wnw_rows_t), ("v", wnw_rows_t), ("rotary", C.c_void_p),
+                ("positions_dev", C.c_void_p), ("axis_stride", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32),
+                ("cuda_stream", C.c_void_p)]
+
+
+class wnw_pages_attend_t(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("batch", wnw_batch_t), ("q", wnw_rows_t), ("out", wnw_rows_t), ("lse_dev", C.c_void_p),
+                ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_int64), ("dtype", C.c_int32), ("causal", C.c_int32),
+                ("softmax_scale", C.c_float), ("reserved", C.c_int32), ("cuda_stream", C.c_void_p)]
+
+
 class WnwError(RuntimeError):
     def __init__(self, status: int, what: str):
         self.status = status
@@ -115,10 +134,10 @@ _SIGNATURES = {
     "wnw_attend_static": [_vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32, C.c_float, _i32, _vp],
     "wnw_attend_static_status": [_i32, _vp, C.POINTER(_i32)],
     "wnw_rotary_init": [C.POINTER(wnw_rotary_t), _i32, C.c_double, C.POINTER(_i32), _i32, _i32, _i32],
-    "wnw_rotate": [_vp, _vp, C.c_int64, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _i32, _i32, _vp],
-    "wnw_pages_write": [_vp, _vp, _vp, _vp, _i32, _vp, _vp, C.c_int64, _vp],
-    "wnw_pages_read": [_vp, _vp, _vp, _vp, _i32, _vp],
-    "wnw_pages_attend": [_vp, _vp, _vp, _vp, _vp, _i32, _i32, C.c_float, _vp, C.c_int64, _vp],
+    "wnw_rotate": [_vp],
+    "wnw_pages_write": [_vp],
+    "wnw_pages_read": [_vp],
+    "wnw_pages_attend": [_vp],
     "wnw_pages_attend_workspace": [_vp, _i32, C.POINTER(C.c_int64)],
 }
 
@@ -461,47 +480,46 @@ def wnw_debug_attend_static_cluster(n_tokens: int, n_q_heads: int, n_kv_heads: i
 
 
 # ---- operators around a caller-owned, paged K/V store of eight bits ----
-_dtypes = None    # torch's element types by the library's
+# A decoder makes three of these calls a layer, and what a call costs the host bounds small batches: the arguments of a call are packed
+# into its struct at once (the layouts of the structures above), and each tensor is asked for each of its properties once.
+_ROWS = "QqqiI"
+_BATCH = "QQQiiii"
+_rotate_call = struct.Struct("QQq" + 4 * _ROWS + "iiiiiIQ")
+_rows_call = struct.Struct("Q" + _BATCH + 2 * _ROWS + "QQqiIQ")
+_attend_call = struct.Struct("Q" + _BATCH + 2 * _ROWS + "QQqiifIQ")
+_no_rows = (0, 0, 0, 0, 0)
+_calls = None     # (dtype numbers, int32, float32, raw stream of a device, the four functions)
 
 
-def _dtype(t) -> int:
-    global _dtypes
-    if _dtypes is None:
-        import torch
-        _dtypes = {torch.bfloat16: WNW_DTYPE_BF16, torch.float16: WNW_DTYPE_FP16, torch.float32: WNW_DTYPE_FP32}
-    return _dtypes.get(t.dtype, -1)
-
-
-def _stream_on(stream, device: int) -> Optional[int]:
-    """The given stream, else the current one of the device that the call's tensors are on."""
-    if stream is not None:
-        return int(stream.cuda_stream) or None
+def _prepare_calls():
+    global _calls
     import torch
-    return torch._C._cuda_getCurrentRawStream(device) or None
+    fns = [C.CFUNCTYPE(C.c_int, _vp)((name, lib())) for name in ("wnw_rotate", "wnw_pages_write", "wnw_pages_read", "wnw_pages_attend")]
+    _calls = ({torch.bfloat16: WNW_DTYPE_BF16, torch.float16: WNW_DTYPE_FP16, torch.float32: WNW_DTYPE_FP32}, torch.int32, torch.float32,
+              torch._C._cuda_getCurrentRawStream, *fns)
+    return _calls
 
 
 def _refuse(what: str, why: str):
     raise WnwError(WNW_ERR_INVALID_ARG, f"{what} ({why})")
 
 
-def _rows(t, what: str, dtype=None, device=None, head_dim=None):
-    """A tensor [rows, heads, head_dim] as the library takes it."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or (stride[2] != 1 and shape[2] != 1):
-        _refuse(what, "rows of heads: [rows, heads, head_dim], innermost contiguous")
-    if dtype is not None and t.dtype != dtype:
-        _refuse(what, "tensors of one type")
-    if t.get_device() < 0 or (device is not None and t.get_device() != device):
+def _rows(t, shape, dtype, device: int, what: str):
+    """The fields of a wnw_rows_t for a tensor [rows, heads, head_dim] that has to be of this shape and type, on this device."""
+    if t.shape != shape or t.dtype != dtype:
+        _refuse(what, "rows of heads [rows, heads, head_dim], of one shape and type with their counterparts")
+    if t.get_device() != device or device < 0:
         _refuse(what, "tensors on one CUDA device")
-    if head_dim is not None and shape[2] != head_dim:
-        _refuse(what, "head_dim")
-    return wnw_rows_t(t.data_ptr(), stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else 0, shape[1], 0)
+    n, heads, d = shape
+    row, head, one = t.stride()
+    if one != 1 and d != 1:
+        _refuse(what, "heads contiguous")
+    return t.data_ptr(), row if n > 1 else 0, head if heads > 1 else 0, heads, 0
 
 
-def _ints(t, what: str, name: str, device: int, dims: int):
-    import torch
-    if t.dtype != torch.int32 or t.dim() != dims or t.get_device() != device or (t.numel() and t.stride(-1) != 1):
-        _refuse(what, f"{name}: int32, {dims}-dimensional, innermost contiguous, on the device of the others")
+def _ints(t, shape, what: str, name: str, device: int):
+    if t.dtype != _calls[1] or t.shape != shape or t.get_device() != device:
+        _refuse(what, f"{name}: int32 of the batch's shape, on the device of the others")
     return t
 
 
@@ -517,35 +535,42 @@ def wnw_rotary_init(n_pairs: int, base: float, sections: Optional[Sequence[int]]
 
 def _positions(positions, rotary, n_rows: int, device: int, what: str):
     """[axes, rows], or [rows] for one axis; returns (pointer, elements between the axes)."""
-    if positions.dim() == 1:
+    axes = rotary.n_axes
+    if axes == 1 and positions.dim() == 1:
         positions = positions.unsqueeze(0)
-    _ints(positions, what, "positions", device, 2)
-    if tuple(positions.shape) != (rotary.n_axes, n_rows):
-        _refuse(what, "positions: one per axis and row")
-    return positions.data_ptr(), positions.stride(0)
+    _ints(positions, (axes, n_rows), what, "positions, one per axis and row", device)
+    axis_stride, one = positions.stride()
+    if one != 1 and n_rows > 1:
+        _refuse(what, "positions: innermost contiguous")
+    return positions.data_ptr(), axis_stride
 
 
 def wnw_rotate(rotary, positions, q, q_out, k=None, k_out=None, inverse=False, stream=None):
     """q, k: [n_tokens, heads, head_dim] bf16, fp16 or fp32 CUDA tensors, any strides with the innermost contiguous; q_out and
     k_out may be q and k.  positions: int32 [n_axes, n_tokens].  inverse: the gradient of the turn."""
-    device, n, head_dim = q.get_device(), q.shape[0], q.shape[-1]
-    rows = [_rows(q, "wnw_rotate"), _rows(q_out, "wnw_rotate", q.dtype, device, head_dim)]
-    if q_out.shape != q.shape or (k is None) != (k_out is None):
-        _refuse("wnw_rotate", "an output of the shape of its input")
-    if k is not None:
-        if k.shape[0] != n or k_out.shape != k.shape:
-            _refuse("wnw_rotate", "as many keys as queries, an output of the shape of its input")
-        rows += [_rows(k, "wnw_rotate", q.dtype, device, head_dim), _rows(k_out, "wnw_rotate", q.dtype, device, head_dim)]
-    at, axis_stride = _positions(positions, rotary, n, device, "wnw_rotate")
-    refs = [C.byref(x) for x in rows] + [None] * (4 - len(rows))
-    _ck(lib().wnw_rotate(C.byref(rotary), at, axis_stride, n, head_dim, _dtype(q), *refs, int(inverse), device, _stream_on(stream, device)),
-        "wnw_rotate")
+    dtypes, _, _, raw_stream, call = (_calls or _prepare_calls())[:5]
+    what, device, shape, dtype = "wnw_rotate", q.get_device(), q.shape, q.dtype
+    if len(shape) != 3 or (k is None) != (k_out is None):
+        _refuse(what, "rows of heads: [n_tokens, heads, head_dim], an output for each input")
+    rq, ro = _rows(q, shape, dtype, device, what), _rows(q_out, shape, dtype, device, what)
+    if k is None:
+        rk = rko = _no_rows
+    else:
+        shape_k = k.shape
+        if len(shape_k) != 3 or shape_k[0] != shape[0] or shape_k[2] != shape[2]:
+            _refuse(what, "as many keys as queries, of one head_dim")
+        rk, rko = _rows(k, shape_k, dtype, device, what), _rows(k_out, shape_k, dtype, device, what)
+    at, axis_stride = _positions(positions, rotary, shape[0], device, what)
+    rc = call(_rotate_call.pack(C.addressof(rotary), at, axis_stride, *rq, *ro, *rk, *rko, shape[0], shape[2], dtypes.get(dtype, -1),
+                                1 if inverse else 0, device, 0, raw_stream(device) if stream is None else stream.cuda_stream))
+    if rc:
+        raise WnwError(rc, what)
 
 
 def wnw_pages(codes, scales, status=None) -> wnw_pages_t:
     """The handle of a store: codes [n_pages, n_kv_heads, 2, page_tokens, head_dim], float8_e4m3fn (or uint8, taken as that) or int8;
     scales float32 [n_pages, n_kv_heads, 2]; status: an int32 CUDA tensor that WNW_PAGES_* bits are OR-ed into.  Pages may lie
-    apart; what is inside a page is contiguous.  The tensors must outlive the handle."""
+    apart; what is inside a page is contiguous.  The handle keeps the tensors alive."""
     import torch
     formats = {torch.float8_e4m3fn: WNW_PAGES_E4M3, torch.uint8: WNW_PAGES_E4M3, torch.int8: WNW_PAGES_INT8}
     if codes.dtype not in formats or codes.dim() != 5 or codes.shape[2] != 2:
@@ -558,49 +583,62 @@ def wnw_pages(codes, scales, status=None) -> wnw_pages_t:
         _refuse("wnw_pages", "a page is contiguous")
     if status is not None and (status.dtype != torch.int32 or status.numel() < 1 or status.get_device() != device):
         _refuse("wnw_pages", "status: an int32 tensor on the codes' CUDA device")
-    return wnw_pages_t(codes.data_ptr(), scales.data_ptr(), codes.stride(0) if n > 1 else 0, scales.stride(0) if n > 1 else 0, n, t, h, d,
-                       formats[codes.dtype], device, _ptr(status))
+    pages = wnw_pages_t(codes.data_ptr(), scales.data_ptr(), codes.stride(0) if n > 1 else 0, scales.stride(0) if n > 1 else 0, n, t, h, d,
+                        formats[codes.dtype], device, _ptr(status))
+    pages.tensors = (codes, scales, status)
+    return pages
 
 
-def _batch(pages, page_table, lengths, row_starts, n_rows: int, max_rows: int, what: str):
-    device, n = pages.device, lengths.shape[0]
-    _ints(page_table, what, "page_table", device, 2)
-    _ints(lengths, what, "lengths", device, 1)
-    _ints(row_starts, what, "row_starts", device, 1)
-    if page_table.shape[0] != n or row_starts.shape[0] != n + 1:
-        _refuse(what, "page_table, lengths and row_starts of one batch")
-    stride = page_table.stride(0) if n > 1 else page_table.shape[1]
-    if stride < page_table.shape[1]:
-        _refuse(what, "page_table: sequences apart from one another")
-    return wnw_batch_t(page_table.data_ptr(), lengths.data_ptr(), row_starts.data_ptr(), stride, n, n_rows, max_rows)
-
-
-def _kv_rows(pages, k, v, what: str):
-    if k.shape != v.shape:
-        _refuse(what, "k and v of one shape")
-    return _rows(k, what, None, pages.device, pages.head_dim), _rows(v, what, k.dtype, pages.device, pages.head_dim)
+def _batch(page_table, lengths, row_starts, device: int, n_rows: int, max_rows: int, what: str):
+    """The fields of a wnw_batch_t."""
+    shape = page_table.shape
+    if len(shape) != 2:
+        _refuse(what, "page_table: [sequences, pages]")
+    n, width = shape
+    stride, one = page_table.stride()
+    _ints(page_table, shape, what, "page_table", device)
+    _ints(lengths, (n,), what, "lengths", device)
+    _ints(row_starts, (n + 1,), what, "row_starts", device)
+    if n < 2:
+        stride = width
+    if (one != 1 and width > 1) or stride < width or (n > 1 and (lengths.stride(0) != 1 or row_starts.stride(0) != 1)):
+        _refuse(what, "page_table, lengths and row_starts: contiguous, sequences apart from one another")
+    return page_table.data_ptr(), lengths.data_ptr(), row_starts.data_ptr(), stride, n, n_rows, max_rows
 
 
 def wnw_pages_write(pages, page_table, lengths, row_starts, k, v, rotary=None, positions=None, max_rows=0, stream=None):
     """k, v: [n_rows, n_kv_heads, head_dim] bf16 or fp16; row i of sequence s becomes its token lengths[s] + i.  With rotary and
     positions (int32 [n_axes, n_rows]) the keys are turned on the way."""
-    rk, rv = _kv_rows(pages, k, v, "wnw_pages_write")
-    batch = _batch(pages, page_table, lengths, row_starts, k.shape[0], max_rows, "wnw_pages_write")
-    at, axis_stride = None, 0
+    dtypes, _, _, raw_stream, _, call = (_calls or _prepare_calls())[:6]
+    what, device, shape, dtype = "wnw_pages_write", pages.device, k.shape, k.dtype
+    if len(shape) != 3 or shape[2] != pages.head_dim:
+        _refuse(what, "k and v: [n_rows, n_kv_heads, head_dim]")
+    rk, rv = _rows(k, shape, dtype, device, what), _rows(v, shape, dtype, device, what)
+    batch = _batch(page_table, lengths, row_starts, device, shape[0], max_rows, what)
+    plan = at = axis_stride = 0
     if (rotary is None) != (positions is None):
-        _refuse("wnw_pages_write", "rotary and positions go together")
+        _refuse(what, "rotary and positions go together")
     if rotary is not None:
-        at, axis_stride = _positions(positions, rotary, k.shape[0], pages.device, "wnw_pages_write")
-    _ck(lib().wnw_pages_write(C.byref(pages), C.byref(batch), C.byref(rk), C.byref(rv), _dtype(k), None if rotary is None else C.byref(rotary),
-                              at, axis_stride, _stream_on(stream, pages.device)), "wnw_pages_write")
+        plan = C.addressof(rotary)
+        at, axis_stride = _positions(positions, rotary, shape[0], device, what)
+    rc = call(_rows_call.pack(C.addressof(pages), *batch, *rk, *rv, plan, at, axis_stride, dtypes.get(dtype, -1), 0,
+                              raw_stream(device) if stream is None else stream.cuda_stream))
+    if rc:
+        raise WnwError(rc, what)
 
 
 def wnw_pages_read(pages, page_table, lengths, row_starts, k, v, max_rows=0, stream=None):
     """Tokens lengths[s], lengths[s] + 1, ... of every sequence into its rows of k and v [n_rows, n_kv_heads, head_dim]."""
-    rk, rv = _kv_rows(pages, k, v, "wnw_pages_read")
-    batch = _batch(pages, page_table, lengths, row_starts, k.shape[0], max_rows, "wnw_pages_read")
-    _ck(lib().wnw_pages_read(C.byref(pages), C.byref(batch), C.byref(rk), C.byref(rv), _dtype(k), _stream_on(stream, pages.device)),
-        "wnw_pages_read")
+    dtypes, _, _, raw_stream, _, _, call = (_calls or _prepare_calls())[:7]
+    what, device, shape, dtype = "wnw_pages_read", pages.device, k.shape, k.dtype
+    if len(shape) != 3 or shape[2] != pages.head_dim:
+        _refuse(what, "k and v: [n_rows, n_kv_heads, head_dim]")
+    rk, rv = _rows(k, shape, dtype, device, what), _rows(v, shape, dtype, device, what)
+    batch = _batch(page_table, lengths, row_starts, device, shape[0], max_rows, what)
+    rc = call(_rows_call.pack(C.addressof(pages), *batch, *rk, *rv, 0, 0, 0, dtypes.get(dtype, -1), 0,
+                              raw_stream(device) if stream is None else stream.cuda_stream))
+    if rc:
+        raise WnwError(rc, what)
 
 
 def wnw_pages_attend_workspace(pages, n_q_heads: int) -> int:
@@ -614,14 +652,20 @@ def wnw_pages_attend(pages, page_table, lengths, row_starts, q, out, workspace, 
                      stream=None):
     """q, out: [n_rows, n_q_heads, head_dim] bf16 or fp16; lse: None or float32 [n_rows, n_q_heads]; workspace: a CUDA tensor of
     wnw_pages_attend_workspace bytes."""
-    device, what = pages.device, "wnw_pages_attend"
-    rq, ro = _rows(q, what, None, device, pages.head_dim), _rows(out, what, q.dtype, device, pages.head_dim)
-    if q.shape != out.shape:
-        _refuse(what, "an output of the queries' shape")
-    batch = _batch(pages, page_table, lengths, row_starts, q.shape[0], max_rows, what)
-    if lse is not None and (str(lse.dtype) != "torch.float32" or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.get_device() != device):
-        _refuse(what, "lse: float32 [n_rows, n_q_heads], contiguous")
+    dtypes, _, float32, raw_stream, _, _, _, call = _calls or _prepare_calls()
+    what, device, shape, dtype = "wnw_pages_attend", pages.device, q.shape, q.dtype
+    if len(shape) != 3 or shape[2] != pages.head_dim:
+        _refuse(what, "q and out: [n_rows, n_q_heads, head_dim]")
+    rq, ro = _rows(q, shape, dtype, device, what), _rows(out, shape, dtype, device, what)
+    batch = _batch(page_table, lengths, row_starts, device, shape[0], max_rows, what)
+    to_lse = 0
+    if lse is not None:
+        if lse.dtype != float32 or lse.shape != shape[:2] or not lse.is_contiguous() or lse.get_device() != device:
+            _refuse(what, "lse: float32 [n_rows, n_q_heads], contiguous")
+        to_lse = lse.data_ptr()
     if workspace.get_device() != device or not workspace.is_contiguous():
         _refuse(what, "workspace: contiguous, on the pages' device")
-    _ck(lib().wnw_pages_attend(C.byref(pages), C.byref(batch), C.byref(rq), C.byref(ro), _ptr(lse), _dtype(q), int(causal), softmax_scale,
-                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_on(stream, device)), what)
+    rc = call(_attend_call.pack(C.addressof(pages), *batch, *rq, *ro, to_lse, workspace.data_ptr(), workspace.nbytes, dtypes.get(dtype, -1),
+                                1 if causal else 0, softmax_scale, 0, raw_stream(device) if stream is None else stream.cuda_stream))
+    if rc:
+        raise WnwError(rc, what)

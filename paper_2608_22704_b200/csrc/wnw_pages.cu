@@ -276,11 +276,13 @@ template <typename T> cudaError_t launch_read(const ReadArgs &a, int d, int fmt,
   return cudaGetLastError();
 }
 
-wnw_status_t check_kv_rows(const wnw_pages_t *p, const wnw_batch_t *b, const wnw_rows_t *k, const wnw_rows_t *v, int dtype) {
-  if (!k || !v) return WNW_ERR_INVALID_ARG;
-  if (dtype != WNW_DTYPE_BF16 && dtype != WNW_DTYPE_FP16) return WNW_ERR_UNSUPPORTED;
-  for (const wnw_rows_t *r : {k, v})
-    if (r->n_heads != p->n_kv_heads || (b->n_rows && (!r->dev || !pg_vector_rows(*r, dtype)))) return WNW_ERR_INVALID_ARG;
+wnw_status_t check_rows_call(const wnw_pages_rows_t *c, PagesView *pv, BatchView *bv) {
+  if (!c) return WNW_ERR_INVALID_ARG;
+  const wnw_status_t rc = pg_view(c->pages, &c->batch, pv, bv);
+  if (rc != WNW_OK) return rc;
+  if (c->dtype != WNW_DTYPE_BF16 && c->dtype != WNW_DTYPE_FP16) return WNW_ERR_UNSUPPORTED;
+  for (const wnw_rows_t *r : {&c->k, &c->v})
+    if (r->n_heads != c->pages->n_kv_heads || (c->batch.n_rows && (!r->dev || !pg_vector_rows(*r, c->dtype)))) return WNW_ERR_INVALID_ARG;
   return WNW_OK;
 }
 
@@ -329,45 +331,43 @@ wnw_status_t pg_sms(int device, int *n) {
 
 using namespace wnw;
 
-extern "C" wnw_status_t wnw_pages_write(const wnw_pages_t *pages, const wnw_batch_t *batch, const wnw_rows_t *k, const wnw_rows_t *v,
-                                        int32_t dtype, const wnw_rotary_t *rotary, const int32_t *positions_dev, int64_t axis_stride,
-                                        void *cuda_stream) {
+extern "C" wnw_status_t wnw_pages_write(const wnw_pages_rows_t *call) {
   WriteArgs a;
-  wnw_status_t rc = pg_view(pages, batch, &a.pv, &a.bv);
-  if (rc != WNW_OK || (rc = check_kv_rows(pages, batch, k, v, dtype)) != WNW_OK) return rc;
+  wnw_status_t rc = check_rows_call(call, &a.pv, &a.bv);
+  if (rc != WNW_OK) return rc;
   a.rot.n_pairs = 0;
-  if (rotary) {
-    if ((rc = rotary_view(rotary, pages->head_dim, 0, &a.rot)) != WNW_OK) return rc;
+  if (call->rotary) {
+    if ((rc = rotary_view(call->rotary, call->pages->head_dim, 0, &a.rot)) != WNW_OK) return rc;
     if (a.rot.n_pairs % 8) return WNW_ERR_UNSUPPORTED;
-    if (batch->n_rows && (!positions_dev || (uintptr_t)positions_dev % 4)) return WNW_ERR_INVALID_ARG;
+    if (call->batch.n_rows && (!call->positions_dev || (uintptr_t)call->positions_dev % 4)) return WNW_ERR_INVALID_ARG;
   }
-  a.positions = positions_dev;
-  a.axis_stride = axis_stride;
-  a.in[0] = rows_view(*k);
-  a.in[1] = rows_view(*v);
-  if (!batch->n_seqs || !batch->n_rows) return WNW_OK;
-  OnDevice on(pages->device);
+  a.positions = call->positions_dev;
+  a.axis_stride = call->axis_stride;
+  a.in[0] = rows_view(call->k);
+  a.in[1] = rows_view(call->v);
+  if (!call->batch.n_seqs || !call->batch.n_rows) return WNW_OK;
+  OnDevice on(call->pages->device);
   if (!on.ok) return WNW_ERR_CUDA;
-  const dim3 grid(pages_touched(*batch, pages->page_tokens), 2 * pages->n_kv_heads, batch->n_seqs);
-  const cudaStream_t st = (cudaStream_t)cuda_stream;
-  const cudaError_t e = dtype == WNW_DTYPE_BF16 ? launch_write<__nv_bfloat16>(a, pages->head_dim, pages->format, grid, st)
-                                                : launch_write<__half>(a, pages->head_dim, pages->format, grid, st);
+  const dim3 grid(pages_touched(call->batch, a.pv.T), 2 * a.pv.H, call->batch.n_seqs);
+  const cudaStream_t st = (cudaStream_t)call->cuda_stream;
+  const int d = call->pages->head_dim, fmt = call->pages->format;
+  const cudaError_t e = call->dtype == WNW_DTYPE_BF16 ? launch_write<__nv_bfloat16>(a, d, fmt, grid, st) : launch_write<__half>(a, d, fmt, grid, st);
   return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
 }
 
-extern "C" wnw_status_t wnw_pages_read(const wnw_pages_t *pages, const wnw_batch_t *batch, const wnw_rows_t *k, const wnw_rows_t *v,
-                                       int32_t dtype, void *cuda_stream) {
+extern "C" wnw_status_t wnw_pages_read(const wnw_pages_rows_t *call) {
   ReadArgs a;
-  wnw_status_t rc = pg_view(pages, batch, &a.pv, &a.bv);
-  if (rc != WNW_OK || (rc = check_kv_rows(pages, batch, k, v, dtype)) != WNW_OK) return rc;
-  a.out[0] = rows_view(*k);
-  a.out[1] = rows_view(*v);
-  if (!batch->n_seqs || !batch->n_rows) return WNW_OK;
-  OnDevice on(pages->device);
+  const wnw_status_t rc = check_rows_call(call, &a.pv, &a.bv);
+  if (rc != WNW_OK) return rc;
+  if (call->rotary) return WNW_ERR_INVALID_ARG;
+  a.out[0] = rows_view(call->k);
+  a.out[1] = rows_view(call->v);
+  if (!call->batch.n_seqs || !call->batch.n_rows) return WNW_OK;
+  OnDevice on(call->pages->device);
   if (!on.ok) return WNW_ERR_CUDA;
-  const dim3 grid(pages_touched(*batch, pages->page_tokens), 2 * pages->n_kv_heads, batch->n_seqs);
-  const cudaStream_t st = (cudaStream_t)cuda_stream;
-  const cudaError_t e = dtype == WNW_DTYPE_BF16 ? launch_read<__nv_bfloat16>(a, pages->head_dim, pages->format, grid, st)
-                                                : launch_read<__half>(a, pages->head_dim, pages->format, grid, st);
+  const dim3 grid(pages_touched(call->batch, a.pv.T), 2 * a.pv.H, call->batch.n_seqs);
+  const cudaStream_t st = (cudaStream_t)call->cuda_stream;
+  const int d = call->pages->head_dim, fmt = call->pages->format;
+  const cudaError_t e = call->dtype == WNW_DTYPE_BF16 ? launch_read<__nv_bfloat16>(a, d, fmt, grid, st) : launch_read<__half>(a, d, fmt, grid, st);
   return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
 }

@@ -647,31 +647,36 @@ extern "C" wnw_status_t wnw_pages_attend_workspace(const wnw_pages_t *pages, int
   return WNW_OK;
 }
 
-extern "C" wnw_status_t wnw_pages_attend(const wnw_pages_t *pages, const wnw_batch_t *batch, const wnw_rows_t *q, const wnw_rows_t *out,
-                                         float *lse_dev, int32_t dtype, int32_t causal, float softmax_scale, void *workspace_dev,
-                                         int64_t workspace_size, void *cuda_stream) {
+extern "C" wnw_status_t wnw_pages_attend(const wnw_pages_attend_t *call) {
+  if (!call) return WNW_ERR_INVALID_ARG;
   AttendArgs a;
   memset(&a, 0, sizeof(a));
+  const wnw_pages_t *pages = call->pages;
+  const wnw_batch_t *batch = &call->batch;
+  const wnw_rows_t &q = call->q, &out = call->out;
+  const float softmax_scale = call->softmax_scale;
+  const int dtype = call->dtype;
   wnw_status_t rc = pg_view(pages, batch, &a.pv, &a.bv);
   if (rc != WNW_OK) return rc;
-  if (!q || !out || (causal & ~1) || q->n_heads != out->n_heads || !(softmax_scale >= 0.f) || std::isinf(softmax_scale)) return WNW_ERR_INVALID_ARG;
+  if ((call->causal & ~1) || q.n_heads != out.n_heads || !(softmax_scale >= 0.f) || std::isinf(softmax_scale)) return WNW_ERR_INVALID_ARG;
   if (dtype != WNW_DTYPE_BF16 && dtype != WNW_DTYPE_FP16) return WNW_ERR_UNSUPPORTED;
-  if ((rc = check_heads(pages, q->n_heads)) != WNW_OK) return rc;
+  if ((rc = check_heads(pages, q.n_heads)) != WNW_OK) return rc;
   if (!batch->n_seqs || !batch->n_rows) return WNW_OK;
-  if (!q->dev || !out->dev || !pg_vector_rows(*q, dtype) || !pg_vector_rows(*out, dtype) || (uintptr_t)lse_dev % 4) return WNW_ERR_INVALID_ARG;
+  if (!q.dev || !out.dev || !pg_vector_rows(q, dtype) || !pg_vector_rows(out, dtype) || (uintptr_t)call->lse_dev % 4) return WNW_ERR_INVALID_ARG;
   OnDevice on(pages->device);
   int n_sm = 0;
   if (!on.ok || pg_sms(pages->device, &n_sm) != WNW_OK) return WNW_ERR_CUDA;
   size_t rows_at, heads_at;
   const size_t need = workspace_bytes(n_sm, pages->head_dim, &rows_at, &heads_at);
-  if (!workspace_dev || (uintptr_t)workspace_dev % 256 || workspace_size < (int64_t)need) return WNW_ERR_INVALID_ARG;
-  a.q = rows_view(*q);
-  a.out = rows_view(*out);
-  a.lse = lse_dev;
-  a.Hq = q->n_heads;
-  a.g = q->n_heads / pages->n_kv_heads;
+  void *const workspace_dev = call->workspace_dev;
+  if (!workspace_dev || (uintptr_t)workspace_dev % 256 || call->workspace_bytes < (int64_t)need) return WNW_ERR_INVALID_ARG;
+  a.q = rows_view(q);
+  a.out = rows_view(out);
+  a.lse = call->lse_dev;
+  a.Hq = q.n_heads;
+  a.g = q.n_heads / pages->n_kv_heads;
   a.dtype = dtype;
-  a.causal = causal;
+  a.causal = call->causal;
   a.scale_log2 = (float)((softmax_scale > 0.f ? (double)softmax_scale : 1.0 / std::sqrt((double)pages->head_dim)) * 1.4426950408889634);
   a.part_o = (float *)workspace_dev;
   a.part_row = (PartRow *)((char *)workspace_dev + rows_at);
@@ -684,7 +689,7 @@ extern "C" wnw_status_t wnw_pages_attend(const wnw_pages_t *pages, const wnw_bat
   a.rt = prompt ? PP_ROWS / a.g : std::min(nt * 8 / a.g, max_rows);
   // items are counted in 32 bits
   if (((long long)batch->n_rows / a.rt + batch->n_seqs) * pages->n_kv_heads > 1ll << 30) return WNW_ERR_CAPACITY;
-  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const cudaStream_t st = (cudaStream_t)call->cuda_stream;
   cudaError_t e;
   if (prompt) {
     e = launch_prompt(a, d, pages->format, n_sm, pages->device, st);

@@ -170,20 +170,19 @@ extern "C" wnw_status_t wnw_rotary_init(wnw_rotary_t *rotary, int32_t n_pairs, d
   return WNW_OK;
 }
 
-extern "C" wnw_status_t wnw_rotate(const wnw_rotary_t *rotary, const int32_t *positions_dev, int64_t axis_stride, int32_t n_tokens,
-                                   int32_t head_dim, int32_t dtype, const wnw_rows_t *q, const wnw_rows_t *q_out, const wnw_rows_t *k,
-                                   const wnw_rows_t *k_out, int32_t inverse, int32_t device, void *cuda_stream) {
-  if (!rotary || !q || !q_out || !k != !k_out || n_tokens < 0 || (inverse & ~1)) return WNW_ERR_INVALID_ARG;
+extern "C" wnw_status_t wnw_rotate(const wnw_rotate_t *call) {
+  if (!call || !call->rotary || !call->k.dev != !call->k_out.dev || call->n_tokens < 0 || (call->inverse & ~1)) return WNW_ERR_INVALID_ARG;
+  const int n_tokens = call->n_tokens, head_dim = call->head_dim, dtype = call->dtype;
   if (head_dim < 2 || head_dim > 256 || head_dim % 2 || dtype < WNW_DTYPE_BF16 || dtype > WNW_DTYPE_FP32) return WNW_ERR_UNSUPPORTED;
   RotateArgs a;
-  const wnw_status_t rc = rotary_view(rotary, head_dim, inverse, &a.rot);
+  const wnw_status_t rc = rotary_view(call->rotary, head_dim, call->inverse, &a.rot);
   if (rc != WNW_OK) return rc;
   const int size = (int)pg_elem(dtype), n = 16 / size;
   bool vec = a.rot.n_pairs % n == 0;
   a.tail = 0;
   a.n_heads[1] = 0;
-  for (int i = 0; i < (k ? 2 : 1); ++i) {
-    const wnw_rows_t &in = i ? *k : *q, &out = i ? *k_out : *q_out;
+  for (int i = 0; i < (call->k.dev ? 2 : 1); ++i) {
+    const wnw_rows_t &in = i ? call->k : call->q, &out = i ? call->k_out : call->q_out;
     if (in.n_heads < 1 || in.n_heads > 4096 || in.n_heads != out.n_heads) return WNW_ERR_INVALID_ARG;
     if (n_tokens && (!in.dev || !out.dev || (uintptr_t)in.dev % size || (uintptr_t)out.dev % size)) return WNW_ERR_INVALID_ARG;
     vec = vec && pg_vector_rows(in, dtype) && pg_vector_rows(out, dtype);
@@ -194,16 +193,16 @@ extern "C" wnw_status_t wnw_rotate(const wnw_rotary_t *rotary, const int32_t *po
     a.n_heads[i] = in.n_heads;
   }
   if (!n_tokens) return WNW_OK;
-  if (!positions_dev || (uintptr_t)positions_dev % 4) return WNW_ERR_INVALID_ARG;
-  a.positions = positions_dev;
-  a.axis_stride = axis_stride;
+  if (!call->positions_dev || (uintptr_t)call->positions_dev % 4) return WNW_ERR_INVALID_ARG;
+  a.positions = call->positions_dev;
+  a.axis_stride = call->axis_stride;
   a.n_tokens = n_tokens;
   a.head_dim = head_dim;
-  OnDevice on(device);
+  OnDevice on(call->device);
   int n_sm = 0;
-  if (!on.ok || pg_sms(device, &n_sm) != WNW_OK) return WNW_ERR_CUDA;
+  if (!on.ok || pg_sms(call->device, &n_sm) != WNW_OK) return WNW_ERR_CUDA;
   a.tokens_per_cta = std::max(1, std::min(16, n_tokens / (n_sm * 8)));
-  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const cudaStream_t st = (cudaStream_t)call->cuda_stream;
   const cudaError_t e = dtype == WNW_DTYPE_BF16 ? launch<__nv_bfloat16>(a, vec, st) : dtype == WNW_DTYPE_FP16 ? launch<__half>(a, vec, st)
                                                                                                               : launch<float>(a, vec, st);
   return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;

@@ -49,6 +49,17 @@ def test_scale_brings_the_largest_magnitude_into_the_top_binade(fmt):
 
 
 # ---- refusals: the pointers are never followed ----
+def test_calls_are_packed_as_the_structures_are():
+    from paper_2608_22704_b200 import binding
+    for call, structure in ((binding._rotate_call, wnw.wnw_rotate_t), (binding._rows_call, wnw.wnw_pages_rows_t),
+                            (binding._attend_call, wnw.wnw_pages_attend_t)):
+        assert call.size == C.sizeof(structure)
+    n = iter(range(1, 100))
+    a = wnw.wnw_pages_attend_t.from_buffer_copy(binding._attend_call.pack(*[next(n) for _ in range(26)]))
+    assert (a.pages, a.batch.page_table_dev, a.batch.max_rows, a.q.dev, a.q.n_heads, a.out.row_stride) == (1, 2, 8, 9, 12, 15)
+    assert (a.lse_dev, a.workspace_bytes, a.dtype, a.causal, a.softmax_scale, a.cuda_stream) == (19, 21, 22, 23, 24.0, 26)
+
+
 def _pages(**kw):
     args = dict(codes_dev=1 << 20, scales_dev=1 << 20, page_stride=0, scale_stride=0, n_pages=8, page_tokens=64, n_kv_heads=4, head_dim=128,
                 format=0, device=0, status_dev=None)
@@ -70,12 +81,10 @@ def _rows(heads=4, dim=128, **kw):
 
 def _all(pages=None, batch=None, k=None, v=None, q=None, out=None, dtype=0, causal=1, scale=0.0, workspace=1 << 20, size=1 << 30):
     """The statuses of write, read and attend."""
-    lib = wnw.lib()
-    ref = lambda x, d: C.byref(d if x is None else x)  # noqa: E731
-    p, b = ref(pages, _pages()), ref(batch, _batch())
-    k, v, q, out = ref(k, _rows()), ref(v, _rows()), ref(q, _rows(16)), ref(out, _rows(16))
-    return (lib.wnw_pages_write(p, b, k, v, dtype, None, None, 0, None), lib.wnw_pages_read(p, b, k, v, dtype, None),
-            lib.wnw_pages_attend(p, b, q, out, None, dtype, causal, scale, workspace, size, None))
+    lib, pages, batch = wnw.lib(), pages or _pages(), batch or _batch()
+    rows = C.byref(wnw.wnw_pages_rows_t(C.addressof(pages), batch, k or _rows(), v or _rows(), None, None, 0, dtype, 0, None))
+    call = wnw.wnw_pages_attend_t(C.addressof(pages), batch, q or _rows(16), out or _rows(16), None, workspace, size, dtype, causal, scale, 0, None)
+    return lib.wnw_pages_write(rows), lib.wnw_pages_read(rows), lib.wnw_pages_attend(C.byref(call))
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -119,23 +128,26 @@ def test_nothing_to_do_is_no_error():
 
 def test_null_arguments():
     lib, bad = wnw.lib(), wnw.WNW_ERR_INVALID_ARG
-    p, b, k, q = (C.byref(x) for x in (_pages(), _batch(), _rows(), _rows(16)))
-    for args in ((None, b, k, k), (p, None, k, k), (p, b, None, k), (p, b, k, None)):
-        assert lib.wnw_pages_write(*args, 0, None, None, 0, None) == bad and lib.wnw_pages_read(*args, 0, None) == bad
-    for args in ((None, b, q, q), (p, None, q, q), (p, b, None, q), (p, b, q, None)):
-        assert lib.wnw_pages_attend(*args, None, 0, 1, 0.0, 1 << 20, 1 << 30, None) == bad
-    n = C.c_int64(5)
+    assert lib.wnw_rotate(None) == lib.wnw_pages_write(None) == lib.wnw_pages_read(None) == lib.wnw_pages_attend(None) == bad
+    rows = wnw.wnw_pages_rows_t(None, _batch(), _rows(), _rows(), None, None, 0, 0, 0, None)
+    assert lib.wnw_pages_write(C.byref(rows)) == lib.wnw_pages_read(C.byref(rows)) == bad
+    call = wnw.wnw_pages_attend_t(None, _batch(), _rows(16), _rows(16), None, 1 << 20, 1 << 30, 0, 1, 0.0, 0, None)
+    assert lib.wnw_pages_attend(C.byref(call)) == bad
+    n, p = C.c_int64(5), C.byref(_pages())
     assert lib.wnw_pages_attend_workspace(None, 16, C.byref(n)) == bad and lib.wnw_pages_attend_workspace(p, 16, None) == bad
     assert lib.wnw_pages_attend_workspace(p, 7, C.byref(n)) == bad and n.value == 5
 
 
 def test_rotary_of_a_write():
-    lib = wnw.lib()
-    p, b, k = (C.byref(x) for x in (_pages(), _batch(), _rows()))
-    write = lambda r, at=1 << 20: lib.wnw_pages_write(p, b, k, k, 0, C.byref(r), at, 2, None)  # noqa: E731
+    lib, pages = wnw.lib(), _pages()
+
+    def write(r, at=1 << 20, call=lib.wnw_pages_write):
+        return call(C.byref(wnw.wnw_pages_rows_t(C.addressof(pages), _batch(), _rows(), _rows(), C.addressof(r), at, 2, 0, 0, None)))
+
     assert write(wnw.wnw_rotary_init(65, 1e4)) == wnw.WNW_ERR_INVALID_ARG            # more elements than a head has
     assert write(wnw.wnw_rotary_init(20, 1e4)) == wnw.WNW_ERR_UNSUPPORTED            # not in eights
     assert write(wnw.wnw_rotary_init(64, 1e4), None) == wnw.WNW_ERR_INVALID_ARG
+    assert write(wnw.wnw_rotary_init(64, 1e4), call=lib.wnw_pages_read) == wnw.WNW_ERR_INVALID_ARG
     r = wnw.wnw_rotary_init(64, 1e4)
     r.axis[3] = 1
     assert write(r) == wnw.WNW_ERR_INVALID_ARG                                       # an axis that is not there
@@ -148,8 +160,10 @@ def test_rotate_refusals():
     lib = wnw.lib()
 
     def rotate(r=None, q=None, q_out=None, k=None, k_out=None, n=3, d=128, dtype=0, inverse=0, at=1 << 20):
-        refs = [None if x is None else C.byref(x) for x in (q or _rows(), q_out or _rows(), k, k_out)]
-        return lib.wnw_rotate(C.byref(r or wnw.wnw_rotary_init(d // 2 if 0 < d <= 256 else 1, 1e4)), at, n, n, d, dtype, *refs, inverse, 0, None)
+        none = _rows(dev=None)
+        r = r or wnw.wnw_rotary_init(d // 2 if 0 < d <= 256 else 1, 1e4)
+        return lib.wnw_rotate(C.byref(wnw.wnw_rotate_t(C.addressof(r), at, n, q or _rows(), q_out or _rows(), k or none, k_out or none, n, d, dtype, inverse,
+                                                       0, 0, None)))
 
     bad, unsup = wnw.WNW_ERR_INVALID_ARG, wnw.WNW_ERR_UNSUPPORTED
     assert rotate(n=-1) == bad and rotate(inverse=2) == bad and rotate(at=None) == bad
