@@ -83,6 +83,8 @@ __global__ void __launch_bounds__(THREADS) wnw_pages_write_kernel(const __grid_c
   __shared__ uint32_t red[16];
   const PagesView &pv = a.pv;
   const int s = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1, nt = THREADS;
+  pg_let_next_start();
+  pg_wait_for_stream();
   const Span sp = span_of(pv, a.bv, s);
   if (sp.first >= sp.end) return;
   const bool turn = a.rot.n_pairs && which == 0;
@@ -213,7 +215,9 @@ template <typename T, int D, int FMT>
 __global__ void __launch_bounds__(256) wnw_pages_read_kernel(const __grid_constant__ ReadArgs a) {
   constexpr int UPR = D / 16;
   const PagesView &pv = a.pv;
-  const int s = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1, nt = blockDim.x;
+  const int s = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1, nt = 256;
+  pg_let_next_start();
+  pg_wait_for_stream();
   const Span sp = span_of(pv, a.bv, s);
   if (sp.first >= sp.end) return;
   const int page0 = sp.first / pv.T, n_touched = (sp.end - 1) / pv.T - page0 + 1;
@@ -256,24 +260,17 @@ int pages_touched(const wnw_batch_t &b, int T) {
 
 template <typename T, int D, int FMT> cudaError_t launch_write(const WriteArgs &a, dim3 grid, cudaStream_t st) {
   const int units = a.pv.T * (D / 16);
-  if (units <= 512) wnw_pages_write_kernel<T, D, FMT, 2, 256><<<grid, 256, 0, st>>>(a);
-  else if (units <= 1024) wnw_pages_write_kernel<T, D, FMT, 4, 256><<<grid, 256, 0, st>>>(a);
-  else wnw_pages_write_kernel<T, D, FMT, 4, 512><<<grid, 512, 0, st>>>(a);
-  return cudaGetLastError();
+  if (units <= 512) return pg_launch(wnw_pages_write_kernel<T, D, FMT, 2, 256>, grid, 256, 0, st, a);
+  if (units <= 1024) return pg_launch(wnw_pages_write_kernel<T, D, FMT, 4, 256>, grid, 256, 0, st, a);
+  return pg_launch(wnw_pages_write_kernel<T, D, FMT, 4, 512>, grid, 512, 0, st, a);
 }
 template <typename T> cudaError_t launch_write(const WriteArgs &a, int d, int fmt, dim3 grid, cudaStream_t st) {
   if (d == 64) return fmt == WNW_PAGES_E4M3 ? launch_write<T, 64, WNW_PAGES_E4M3>(a, grid, st) : launch_write<T, 64, WNW_PAGES_INT8>(a, grid, st);
   return fmt == WNW_PAGES_E4M3 ? launch_write<T, 128, WNW_PAGES_E4M3>(a, grid, st) : launch_write<T, 128, WNW_PAGES_INT8>(a, grid, st);
 }
 template <typename T> cudaError_t launch_read(const ReadArgs &a, int d, int fmt, dim3 grid, cudaStream_t st) {
-  if (d == 64) {
-    if (fmt == WNW_PAGES_E4M3) wnw_pages_read_kernel<T, 64, WNW_PAGES_E4M3><<<grid, 256, 0, st>>>(a);
-    else wnw_pages_read_kernel<T, 64, WNW_PAGES_INT8><<<grid, 256, 0, st>>>(a);
-  } else {
-    if (fmt == WNW_PAGES_E4M3) wnw_pages_read_kernel<T, 128, WNW_PAGES_E4M3><<<grid, 256, 0, st>>>(a);
-    else wnw_pages_read_kernel<T, 128, WNW_PAGES_INT8><<<grid, 256, 0, st>>>(a);
-  }
-  return cudaGetLastError();
+  if (d == 64) return pg_launch(fmt == WNW_PAGES_E4M3 ? wnw_pages_read_kernel<T, 64, WNW_PAGES_E4M3> : wnw_pages_read_kernel<T, 64, WNW_PAGES_INT8>, grid, 256, 0, st, a);
+  return pg_launch(fmt == WNW_PAGES_E4M3 ? wnw_pages_read_kernel<T, 128, WNW_PAGES_E4M3> : wnw_pages_read_kernel<T, 128, WNW_PAGES_INT8>, grid, 256, 0, st, a);
 }
 
 wnw_status_t check_rows_call(const wnw_pages_rows_t *c, PagesView *pv, BatchView *bv) {

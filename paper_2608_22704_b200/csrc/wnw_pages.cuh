@@ -90,6 +90,27 @@ wnw_status_t pg_view(const wnw_pages_t *p, const wnw_batch_t *b, PagesView *pv, 
 wnw_status_t rotary_view(const wnw_rotary_t *r, int head_dim, int inverse, RotaryView *v);
 inline RowsView rows_view(const wnw_rows_t &r) { return RowsView{(unsigned char *)r.dev, (long long)r.row_stride, (long long)r.head_stride}; }
 
+// ---- launches that start while their predecessor on the stream ends ----
+// The next launch may be brought onto the SMs from here on; it waits itself before it touches anything.
+__device__ __forceinline__ void pg_let_next_start() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
+// Everything before on the stream has completed.  By every CTA, before its first access to memory: then "completed" holds along chains.
+__device__ __forceinline__ void pg_wait_for_stream() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
+template <typename... P, typename... A> cudaError_t pg_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A &...args) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+  if (e != cudaSuccess) cudaGetLastError();
+  return e;
+}
+
 // SMs of a device, asked for once.
 wnw_status_t pg_sms(int device, int *n);
 

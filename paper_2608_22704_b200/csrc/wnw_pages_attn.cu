@@ -128,7 +128,7 @@ __device__ __forceinline__ long long lay_out(const AttendArgs &a, long long *gra
   return gbase;
 }
 // Granules that a CTA takes: equal stretches, none shorter than a granule for each warp.
-template <int W> __device__ __forceinline__ long long stretch(long long total, int n_ctas) { return max((long long)W, (total + n_ctas - 1) / n_ctas); }
+template <int W> __device__ __forceinline__ long long stretch(long long total, int n_ctas) { return max((long long)W, quotient(total + n_ctas - 1, n_ctas)); }
 
 template <int D, int FMT, int NT>
 __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map) {
@@ -153,6 +153,8 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
     asm volatile("prefetch.tensormap [%0];\n" ::"l"(&map) : "memory");
   }
   __syncwarp();
+  pg_let_next_start();
+  pg_wait_for_stream();
   const long long total = lay_out<W>(a, grans, items);
   const long long len_line = stretch<W>(total, gridDim.x), x0 = min(total, blockIdx.x * len_line), x1 = min(total, x0 + len_line);
   if (tid == 0) a.part_head[blockIdx.x] = PartHead{0, 0, 0, 0};
@@ -163,8 +165,8 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
     int lo = 0, hi = a.bv.n_seqs;                       // the last sequence that begins at or before x0 and is not empty
     while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (grans[mid] <= x0) lo = mid; else hi = mid; }
     const int n_it = items[lo + 1] - items[lo];
-    const long long per = (grans[lo + 1] - grans[lo]) / n_it;
-    item0 = items[lo] + (int)((x0 - grans[lo]) / per);
+    const long long per = quotient(grans[lo + 1] - grans[lo], n_it);
+    item0 = items[lo] + (int)quotient(x0 - grans[lo], per);
   }
   const int n_items = items[a.bv.n_seqs];
   // a lane's 16-byte pieces of K row r and V rows 2c, 2c + 1 (and 8 rows on) in a swizzled granule
@@ -187,7 +189,7 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
         int lo = 0, hi = a.bv.n_seqs;
         while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (items[mid] <= item) lo = mid; else hi = mid; }
         const int n_it = items[lo + 1] - items[lo], it = item - items[lo], tiles = n_it / pv.H;
-        const long long per = (grans[lo + 1] - grans[lo]) / n_it, b = grans[lo] + it * per, e = b + per;
+        const long long per = quotient(grans[lo + 1] - grans[lo], n_it), b = grans[lo] + it * per, e = b + per;
         if (b < x1) {
           mine = 1;
           Seg &sg = segs[tid];
@@ -202,7 +204,7 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
           const int last = min(sg.len, a.causal ? sg.end0 + sg.nq - 1 : sg.len);
           sg.need = last > 0 ? (last + PG_GR - 1) / PG_GR : 0;
           sg.slot = b >= x0 && e <= x1 ? -1 : b < x0 ? 0 : 1;
-          sg.n_parts = (int)((e - 1) / len_line - b / len_line + 1);
+          sg.n_parts = (int)(quotient(e - 1, len_line) - quotient(b, len_line) + 1);
         }
       }
       n_seg = __syncthreads_count(mine);
@@ -522,6 +524,8 @@ __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_consta
   constexpr int LANES = D / 4, SPLIT = 128 / LANES;
   __shared__ float4 acc_s[SPLIT][LANES];
   __shared__ float sum_s[SPLIT], red[2][4];
+  pg_let_next_start();
+  pg_wait_for_stream();
   const PartHead ph = a.part_head[blockIdx.x];
   if (ph.n_parts < 2) return;
   const int r0 = max(a.bv.starts[ph.s], 0), n = min(a.bv.starts[ph.s + 1], a.bv.n_rows) - r0, used = a.rt * a.g;
@@ -617,8 +621,7 @@ template <int D, int FMT, int NT> cudaError_t launch(const AttendArgs &a, const 
     if (e != cudaSuccess) return e;
     ready.fetch_or(1ull << device, std::memory_order_release);
   }
-  wnw_pages_attend_kernel<D, FMT, NT><<<n_ctas, Geo<D, NT>::THREADS, smem_bytes<D, NT>(), st>>>(a, map);
-  return cudaGetLastError();
+  return pg_launch(wnw_pages_attend_kernel<D, FMT, NT>, dim3(n_ctas), Geo<D, NT>::THREADS, smem_bytes<D, NT>(), st, a, map);
 }
 template <int D, int FMT> cudaError_t launch(const AttendArgs &a, const CUtensorMap &map, int nt, int n_ctas, int device, cudaStream_t st) {
   return nt == 1 ? launch<D, FMT, 1>(a, map, n_ctas, device, st) : launch<D, FMT, 2>(a, map, n_ctas, device, st);
@@ -702,8 +705,6 @@ extern "C" wnw_status_t wnw_pages_attend(const wnw_pages_attend_t *call) {
   }
   if (e != cudaSuccess) return WNW_ERR_CUDA;
   const dim3 grid(n_sm, prompt ? 16 : a.rt * a.g);
-  if (d == 64) wnw_pages_join_kernel<64><<<grid, 128, 0, st>>>(a);
-  else wnw_pages_join_kernel<128><<<grid, 128, 0, st>>>(a);
-  e = cudaGetLastError();
+  e = pg_launch(d == 64 ? wnw_pages_join_kernel<64> : wnw_pages_join_kernel<128>, grid, 128, 0, st, a);
   return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
 }

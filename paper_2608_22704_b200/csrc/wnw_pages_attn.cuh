@@ -57,6 +57,11 @@ template <int FMT> __device__ __forceinline__ void to_half(uint32_t w, uint32_t 
 }
 
 
+// x / y of numbers that are not negative; a 64-bit division takes some hundred instructions, and hardly ever is one needed
+__device__ __forceinline__ long long quotient(long long x, long long y) {
+  return ((x | y) >> 32) ? x / y : (long long)((uint32_t)x / (uint32_t)y);
+}
+
 // The attention of many query rows (wnw_pages_prompt.cu): 128-row tiles, two at a time.
 constexpr int PP_ROWS = 128, PP_BLOCKS = 2;
 cudaError_t launch_prompt(const AttendArgs &a, int head_dim, int format, int n_ctas, int device, cudaStream_t st);

@@ -345,8 +345,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
     asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;\n" ::"r"(smem_u32(&sh.begun)) : "memory");
     fence_smem();
     sh.dead = 0;
-    a.part_head[blockIdx.x] = PartHead{0, 0, 0, 0};
   }
+  pg_let_next_start();
+  pg_wait_for_stream();
+  if (tid == 0) a.part_head[blockIdx.x] = PartHead{0, 0, 0, 0};
   const long long total = lay_out(a, sh);              // (its barriers order the above too)
   const long long len_line = (total + gridDim.x - 1) / gridDim.x, x0 = min(total, blockIdx.x * len_line), x1 = min(total, x0 + len_line);
   if (x0 >= x1) return;
@@ -710,8 +712,7 @@ template <int D, int FMT> cudaError_t launch(const AttendArgs &a, int n_ctas, in
     if (e != cudaSuccess) return e;
     ready.fetch_or(1ull << device, std::memory_order_release);
   }
-  wnw_pages_prompt_kernel<D, FMT><<<n_ctas, PP_THREADS, smem_bytes<D>(), st>>>(a);
-  return cudaGetLastError();
+  return pg_launch(wnw_pages_prompt_kernel<D, FMT>, dim3(n_ctas), PP_THREADS, smem_bytes<D>(), st, a);
 }
 
 }  // namespace

@@ -61,6 +61,8 @@ template <> struct Vec<float> {
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(ROT_THREADS) wnw_rotate_kernel(const __grid_constant__ RotateArgs a) {
   extern __shared__ float2 cs[];                        // [tokens_per_cta][n_pairs]
+  pg_let_next_start();
+  pg_wait_for_stream();
   const int np = a.rot.n_pairs, t0 = blockIdx.x * a.tokens_per_cta, nt = min(a.tokens_per_cta, a.n_tokens - t0);
   for (int i = threadIdx.x; i < nt * np; i += ROT_THREADS) {
     const int t = i / np, p = i - t * np;
@@ -116,9 +118,7 @@ __global__ void __launch_bounds__(ROT_THREADS) wnw_rotate_kernel(const __grid_co
 template <typename T> cudaError_t launch(const RotateArgs &a, bool vec, cudaStream_t st) {
   const int grid = (a.n_tokens + a.tokens_per_cta - 1) / a.tokens_per_cta;
   const size_t smem = sizeof(float2) * a.tokens_per_cta * a.rot.n_pairs;
-  if (vec) wnw_rotate_kernel<T, true><<<grid, ROT_THREADS, smem, st>>>(a);
-  else wnw_rotate_kernel<T, false><<<grid, ROT_THREADS, smem, st>>>(a);
-  return cudaGetLastError();
+  return pg_launch(vec ? wnw_rotate_kernel<T, true> : wnw_rotate_kernel<T, false>, dim3(grid), ROT_THREADS, smem, st, a);
 }
 
 }  // namespace
