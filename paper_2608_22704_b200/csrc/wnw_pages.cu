@@ -260,17 +260,17 @@ int pages_touched(const wnw_batch_t &b, int T) {
 
 template <typename T, int D, int FMT> cudaError_t launch_write(const WriteArgs &a, dim3 grid, cudaStream_t st) {
   const int units = a.pv.T * (D / 16);
-  if (units <= 512) return pg_launch(wnw_pages_write_kernel<T, D, FMT, 2, 256>, grid, 256, 0, st, a);
-  if (units <= 1024) return pg_launch(wnw_pages_write_kernel<T, D, FMT, 4, 256>, grid, 256, 0, st, a);
-  return pg_launch(wnw_pages_write_kernel<T, D, FMT, 4, 512>, grid, 512, 0, st, a);
+  if (units <= 512) return pg_launch(wnw_pages_write_kernel<T, D, FMT, 2, 256>, grid, 256, 0, st, 0, a);
+  if (units <= 1024) return pg_launch(wnw_pages_write_kernel<T, D, FMT, 4, 256>, grid, 256, 0, st, 0, a);
+  return pg_launch(wnw_pages_write_kernel<T, D, FMT, 4, 512>, grid, 512, 0, st, 0, a);
 }
 template <typename T> cudaError_t launch_write(const WriteArgs &a, int d, int fmt, dim3 grid, cudaStream_t st) {
   if (d == 64) return fmt == WNW_PAGES_E4M3 ? launch_write<T, 64, WNW_PAGES_E4M3>(a, grid, st) : launch_write<T, 64, WNW_PAGES_INT8>(a, grid, st);
   return fmt == WNW_PAGES_E4M3 ? launch_write<T, 128, WNW_PAGES_E4M3>(a, grid, st) : launch_write<T, 128, WNW_PAGES_INT8>(a, grid, st);
 }
 template <typename T> cudaError_t launch_read(const ReadArgs &a, int d, int fmt, dim3 grid, cudaStream_t st) {
-  if (d == 64) return pg_launch(fmt == WNW_PAGES_E4M3 ? wnw_pages_read_kernel<T, 64, WNW_PAGES_E4M3> : wnw_pages_read_kernel<T, 64, WNW_PAGES_INT8>, grid, 256, 0, st, a);
-  return pg_launch(fmt == WNW_PAGES_E4M3 ? wnw_pages_read_kernel<T, 128, WNW_PAGES_E4M3> : wnw_pages_read_kernel<T, 128, WNW_PAGES_INT8>, grid, 256, 0, st, a);
+  if (d == 64) return pg_launch(fmt == WNW_PAGES_E4M3 ? wnw_pages_read_kernel<T, 64, WNW_PAGES_E4M3> : wnw_pages_read_kernel<T, 64, WNW_PAGES_INT8>, grid, 256, 0, st, 0, a);
+  return pg_launch(fmt == WNW_PAGES_E4M3 ? wnw_pages_read_kernel<T, 128, WNW_PAGES_E4M3> : wnw_pages_read_kernel<T, 128, WNW_PAGES_INT8>, grid, 256, 0, st, 0, a);
 }
 
 wnw_status_t check_rows_call(const wnw_pages_rows_t *c, PagesView *pv, BatchView *bv) {

@@ -95,8 +95,9 @@ inline RowsView rows_view(const wnw_rows_t &r) { return RowsView{(unsigned char 
 __device__ __forceinline__ void pg_let_next_start() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
 // Everything before on the stream has completed.  By every CTA, before its first access to memory: then "completed" holds along chains.
 __device__ __forceinline__ void pg_wait_for_stream() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
-template <typename... P, typename... A> cudaError_t pg_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A &...args) {
-  cudaLaunchAttribute attr[1];
+template <typename... P, typename... A>
+cudaError_t pg_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, const A &...args) {   // cluster: CTAs, 0: none
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
@@ -106,6 +107,12 @@ template <typename... P, typename... A> cudaError_t pg_launch(void (*kernel)(P..
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
+  if (cluster) {
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.numAttrs = 2;
+  }
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
   if (e != cudaSuccess) cudaGetLastError();
   return e;

@@ -46,6 +46,13 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ float4 peer(uint32_t at, uint32_t rank) {   // 16 bytes of another CTA of the cluster
+  uint32_t there;
+  float4 x;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(there) : "r"(at), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(there));
+  return x;
+}
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {   // an 8 x 8 matrix of 16-bit elements over the warp
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(x));
@@ -76,8 +83,8 @@ template <int D, int NT> struct Geo {
 };
 template <int D, int NT> constexpr size_t smem_bytes() {
   using G = Geo<D, NT>;
-  return (size_t)G::W * G::S * (G::STAGE + sizeof(uint32_t) + sizeof(uint64_t)) + G::W * NT * 8 * (G::PITCH * 4 + sizeof(PartRow)) + PA_SEGS * sizeof(Seg) +
-         (PG_MAX_SEQS + 1) * (sizeof(long long) + sizeof(int));
+  return (size_t)G::W * G::S * (G::STAGE + sizeof(uint32_t) + sizeof(uint64_t)) + (G::W + 1) * NT * 8 * (G::PITCH * 4 + sizeof(PartRow)) +
+         PA_SEGS * sizeof(Seg) + (PG_MAX_SEQS + 1) * (sizeof(long long) + sizeof(int));
 }
 
 // The line: granules and heads (items) of the sequences before each one.  Returns the granules of all.
@@ -130,15 +137,19 @@ __device__ __forceinline__ long long lay_out(const AttendArgs &a, long long *gra
 // Granules that a CTA takes: equal stretches, none shorter than a granule for each warp.
 template <int W> __device__ __forceinline__ long long stretch(long long total, int n_ctas) { return max((long long)W, quotient(total + n_ctas - 1, n_ctas)); }
 
-template <int D, int FMT, int NT>
+// CLUSTER: no line; cluster i takes KV head i % H of sequence i / H, its CTAs equal shares of the tokens, and their results meet in the
+// cluster's shared memory instead of in the workspace.
+template <int D, int FMT, int NT, bool CLUSTER>
 __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map) {
   using G = Geo<D, NT>;
   constexpr int W = G::W, S = G::S;
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char *ring = smem;
   float *meet = reinterpret_cast<float *>(ring + W * S * G::STAGE);            // [warp][row][PITCH]
-  PartRow *meet_row = reinterpret_cast<PartRow *>(meet + W * NT * 8 * G::PITCH);       // [warp][row]
-  uint64_t *bars = reinterpret_cast<uint64_t *>(meet_row + W * NT * 8);                       // [warp][stage]
+  float *mine_o = meet + W * NT * 8 * G::PITCH;                                        // the CTA's own, for its cluster: [row][PITCH]
+  PartRow *meet_row = reinterpret_cast<PartRow *>(mine_o + NT * 8 * G::PITCH);         // [warp][row]
+  PartRow *mine_row = meet_row + W * NT * 8;
+  uint64_t *bars = reinterpret_cast<uint64_t *>(mine_row + NT * 8);                           // [warp][stage]
   long long *grans = reinterpret_cast<long long *>(bars + W * S);
   Seg *segs = reinterpret_cast<Seg *>(grans + PG_MAX_SEQS + 1);
   int *items = reinterpret_cast<int *>(segs + PA_SEGS);
@@ -155,20 +166,27 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
   __syncwarp();
   pg_let_next_start();
   pg_wait_for_stream();
-  const long long total = lay_out<W>(a, grans, items);
-  const long long len_line = stretch<W>(total, gridDim.x), x0 = min(total, blockIdx.x * len_line), x1 = min(total, x0 + len_line);
-  if (tid == 0) a.part_head[blockIdx.x] = PartHead{0, 0, 0, 0};
-  if (x0 >= x1) return;
-  // the first head of the line
-  int item0 = 0;
-  {
+  long long len_line = 0, x0 = 0, x1 = 0;
+  int item0 = 0, n_items = 0;                           // CLUSTER: the tile of query tokens
+  uint32_t rank = 0, n_ranks = 1;
+  if constexpr (CLUSTER) {
+    asm("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
+    asm("mov.u32 %0, %%cluster_nctarank;\n" : "=r"(n_ranks));
+  } else {
+    const long long total = lay_out<W>(a, grans, items);
+    len_line = stretch<W>(total, gridDim.x);
+    x0 = min(total, blockIdx.x * len_line);
+    x1 = min(total, x0 + len_line);
+    if (tid == 0) a.part_head[blockIdx.x] = PartHead{0, 0, 0, 0};
+    if (x0 >= x1) return;
+    // the first head of the line
     int lo = 0, hi = a.bv.n_seqs;                       // the last sequence that begins at or before x0 and is not empty
     while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (grans[mid] <= x0) lo = mid; else hi = mid; }
     const int n_it = items[lo + 1] - items[lo];
     const long long per = quotient(grans[lo + 1] - grans[lo], n_it);
     item0 = items[lo] + (int)quotient(x0 - grans[lo], per);
+    n_items = items[a.bv.n_seqs];
   }
-  const int n_items = items[a.bv.n_seqs];
   // a lane's 16-byte pieces of K row r and V rows 2c, 2c + 1 (and 8 rows on) in a swizzled granule
   int k_at[G::KC], v_at[2];
 #pragma unroll
@@ -182,35 +200,63 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
     // ---- the next stretches ----
     __syncthreads();
     int n_seg;
-    {
-      int mine = 0;
-      if (tid < PA_SEGS && item0 + tid < n_items) {
-        const int item = item0 + tid;
-        int lo = 0, hi = a.bv.n_seqs;
-        while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (items[mid] <= item) lo = mid; else hi = mid; }
-        const int n_it = items[lo + 1] - items[lo], it = item - items[lo], tiles = n_it / pv.H;
-        const long long per = quotient(grans[lo + 1] - grans[lo], n_it), b = grans[lo] + it * per, e = b + per;
-        if (b < x1) {
-          mine = 1;
-          Seg &sg = segs[tid];
-          const long long f = max(b, x0), l = min(e, x1);
-          sg.s = lo; sg.h = it / tiles; sg.tile = it % tiles;
-          sg.g0 = (int)(f - b); sg.n = (int)(l - f); sg.y0 = (int)(f - x0);
-          const int cap = a.bv.stride * pv.T, r0 = max(a.bv.starts[lo], 0), r1 = min(a.bv.starts[lo + 1], a.bv.n_rows);
-          sg.len = max(0, min(a.bv.lengths[lo], cap));
-          sg.nq = min(a.rt, r1 - r0 - sg.tile * a.rt);
-          sg.row0 = r0 + sg.tile * a.rt;
-          sg.end0 = a.causal ? sg.len - (r1 - r0) + sg.tile * a.rt + 1 : sg.len;
-          const int last = min(sg.len, a.causal ? sg.end0 + sg.nq - 1 : sg.len);
-          sg.need = last > 0 ? (last + PG_GR - 1) / PG_GR : 0;
-          sg.slot = b >= x0 && e <= x1 ? -1 : b < x0 ? 0 : 1;
-          sg.n_parts = (int)(quotient(e - 1, len_line) - quotient(b, len_line) + 1);
-        }
+    if constexpr (CLUSTER) {
+      const int seq = blockIdx.x / n_ranks / pv.H, cap = a.bv.stride * pv.T;
+      const int y0 = a.bv.starts[seq], y1 = a.bv.starts[seq + 1], y2 = a.bv.lengths[seq];
+      const int r0 = max(y0, 0), n = max(0, min(y1, a.bv.n_rows) - r0), len = max(0, min(y2, cap));
+      if (tid == 0 && (y0 < 0 || y1 < y0 || y1 > a.bv.n_rows || y2 < 0 || y2 > cap)) pg_report(pv, WNW_PAGES_BAD_LENGTH);
+      const int first = item0 * a.rt;                   // query token of the sequence
+      if (first >= n) break;                            // (all CTAs of the cluster alike)
+      if (tid == 0) {
+        Seg &sg = segs[0];
+        sg.s = seq; sg.h = blockIdx.x / n_ranks % pv.H; sg.tile = item0;
+        sg.len = len;
+        sg.nq = min(a.rt, n - first);
+        sg.row0 = r0 + first;
+        sg.end0 = a.causal ? len - n + first + 1 : len;
+        const int last = min(len, a.causal ? sg.end0 + sg.nq - 1 : len);
+        sg.need = last > 0 ? (last + PG_GR - 1) / PG_GR : 0;
+        const int share = (sg.need + n_ranks - 1) / n_ranks;
+        sg.g0 = min(sg.need, (int)rank * share);
+        sg.n = min(sg.need - sg.g0, share);
+        sg.y0 = 0;
+        sg.slot = -1;
+        sg.n_parts = 1;
       }
-      n_seg = __syncthreads_count(mine);
+      __syncthreads();
+      n_seg = 1;
+      ++item0;
+    } else {
+      {
+          int mine = 0;
+        if (tid < PA_SEGS && item0 + tid < n_items) {
+          const int item = item0 + tid;
+          int lo = 0, hi = a.bv.n_seqs;
+          while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (items[mid] <= item) lo = mid; else hi = mid; }
+          const int n_it = items[lo + 1] - items[lo], it = item - items[lo], tiles = n_it / pv.H;
+          const long long per = quotient(grans[lo + 1] - grans[lo], n_it), b = grans[lo] + it * per, e = b + per;
+          if (b < x1) {
+            mine = 1;
+            Seg &sg = segs[tid];
+            const long long f = max(b, x0), l = min(e, x1);
+            sg.s = lo; sg.h = it / tiles; sg.tile = it % tiles;
+            sg.g0 = (int)(f - b); sg.n = (int)(l - f); sg.y0 = (int)(f - x0);
+            const int cap = a.bv.stride * pv.T, r0 = max(a.bv.starts[lo], 0), r1 = min(a.bv.starts[lo + 1], a.bv.n_rows);
+            sg.len = max(0, min(a.bv.lengths[lo], cap));
+            sg.nq = min(a.rt, r1 - r0 - sg.tile * a.rt);
+            sg.row0 = r0 + sg.tile * a.rt;
+            sg.end0 = a.causal ? sg.len - (r1 - r0) + sg.tile * a.rt + 1 : sg.len;
+            const int last = min(sg.len, a.causal ? sg.end0 + sg.nq - 1 : sg.len);
+            sg.need = last > 0 ? (last + PG_GR - 1) / PG_GR : 0;
+            sg.slot = b >= x0 && e <= x1 ? -1 : b < x0 ? 0 : 1;
+            sg.n_parts = (int)(quotient(e - 1, len_line) - quotient(b, len_line) + 1);
+          }
+        }
+        n_seg = __syncthreads_count(mine);
+      }
+      more = n_seg == PA_SEGS;                          // (a last round of none costs nothing)
+      item0 += n_seg;
     }
-    more = n_seg == PA_SEGS;                            // (a last round of none costs nothing)
-    item0 += n_seg;
 
     // ---- copies run ahead of the products by S - 1 granules, over the stretches' ends ----
     int p_seg = -1, p_g = 0, p_end = 0, p_cnt = 0, p_stage = 0;
@@ -494,7 +540,10 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
             sum += pr.l * ex2(pr.m - mx);
             acc.x += x.x * by; acc.y += x.y * by; acc.z += x.z * by; acc.w += x.w * by;
           }
-          if (sg.slot < 0) {
+          if (CLUSTER) {
+            *reinterpret_cast<float4 *>(mine_o + j * G::PITCH + d) = acc;
+            if (d == 0) mine_row[j] = PartRow{mx, bx, sum, 0.f};
+          } else if (sg.slot < 0) {
             const float by = sum == 0.f ? 0.f : ex2(bx - mx) / sum;      // (no token: zeros)
             const long long row = sg.row0 + tok;
             const int head = sg.h * a.g + hd;
@@ -511,7 +560,35 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
           }
         }
       }
-      if (tid == 0 && sg.slot == 1) a.part_head[blockIdx.x] = PartHead{sg.s, sg.h, sg.tile, sg.n_parts};
+      if constexpr (CLUSTER) {                          // the CTAs' results meet: each puts together its share of the output
+        asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+        const int used = sg.nq * a.g * (D / 4);         // (rows of real query tokens come first)
+        for (int i = rank * G::THREADS + tid; i < used; i += n_ranks * G::THREADS) {
+          const int j = i / (D / 4), d = i % (D / 4) * 4, tok = j / a.g, head = sg.h * a.g + j - tok * a.g;
+          const uint32_t o_at = (uint32_t)__cvta_generic_to_shared(mine_o + j * G::PITCH + d), r_at = (uint32_t)__cvta_generic_to_shared(mine_row + j);
+          float mx = NOTHING, bx = NOTHING, sum = 0.f;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (uint32_t k = 0; k < n_ranks; ++k) {
+            const float4 pr = peer(r_at, k);
+            mx = fmaxf(mx, pr.x);
+            bx = fmaxf(bx, pr.y);
+          }
+          for (uint32_t k = 0; k < n_ranks; ++k) {
+            const float4 pr = peer(r_at, k), x = peer(o_at, k);
+            const float by = ex2(pr.y - bx);
+            sum += pr.z * ex2(pr.x - mx);
+            acc.x += x.x * by; acc.y += x.y * by; acc.z += x.z * by; acc.w += x.w * by;
+          }
+          const float by = sum == 0.f ? 0.f : ex2(bx - mx) / sum;      // (no token: zeros)
+          const long long row = sg.row0 + tok;
+          unsigned char *p = a.out.p + 2 * (row * a.out.row + head * a.out.head + d);
+          if (a.dtype == WNW_DTYPE_BF16) *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__nv_bfloat16>::put(acc.x * by, acc.y * by), Pair<__nv_bfloat16>::put(acc.z * by, acc.w * by));
+          else *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__half>::put(acc.x * by, acc.y * by), Pair<__half>::put(acc.z * by, acc.w * by));
+          if (a.lse && d == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718055994531f;
+        }
+        asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");   // read by all, free again
+      }
+      if (!CLUSTER && tid == 0 && sg.slot == 1) a.part_head[blockIdx.x] = PartHead{sg.s, sg.h, sg.tile, sg.n_parts};
       __syncthreads();
     }
   }
@@ -614,17 +691,33 @@ bool encode_map(CUtensorMap *map, const PagesView &pv, int d) {
             d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int FMT, int NT> cudaError_t launch(const AttendArgs &a, const CUtensorMap &map, int n_ctas, int device, cudaStream_t st) {
+template <int D, int FMT, int NT, bool CLUSTER>
+cudaError_t launch_form(const AttendArgs &a, const CUtensorMap &map, int n_ctas, int cluster, int device, cudaStream_t st) {
   static std::atomic<unsigned long long> ready{0};       // devices whose kernel has its shared memory
+  const auto kernel = wnw_pages_attend_kernel<D, FMT, NT, CLUSTER>;
   if (!(ready.load(std::memory_order_acquire) >> device & 1)) {
-    const cudaError_t e = cudaFuncSetAttribute(wnw_pages_attend_kernel<D, FMT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D, NT>());
-    if (e != cudaSuccess) return e;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D, NT>());
+    if (e != cudaSuccess) { cudaGetLastError(); return e; }
     ready.fetch_or(1ull << device, std::memory_order_release);
   }
-  return pg_launch(wnw_pages_attend_kernel<D, FMT, NT>, dim3(n_ctas), Geo<D, NT>::THREADS, smem_bytes<D, NT>(), st, a, map);
+  return pg_launch(kernel, dim3(n_ctas), Geo<D, NT>::THREADS, smem_bytes<D, NT>(), st, cluster, a, map);
 }
-template <int D, int FMT> cudaError_t launch(const AttendArgs &a, const CUtensorMap &map, int nt, int n_ctas, int device, cudaStream_t st) {
-  return nt == 1 ? launch<D, FMT, 1>(a, map, n_ctas, device, st) : launch<D, FMT, 2>(a, map, n_ctas, device, st);
+template <int D, int FMT, int NT> cudaError_t launch(const AttendArgs &a, const CUtensorMap &map, int n_ctas, int cluster, int device, cudaStream_t st) {
+  return cluster ? launch_form<D, FMT, NT, true>(a, map, n_ctas, cluster, device, st) : launch_form<D, FMT, NT, false>(a, map, n_ctas, 0, device, st);
+}
+template <int D, int FMT> cudaError_t launch(const AttendArgs &a, const CUtensorMap &map, int nt, int n_ctas, int cluster, int device, cudaStream_t st) {
+  return nt == 1 ? launch<D, FMT, 1>(a, map, n_ctas, cluster, device, st) : launch<D, FMT, 2>(a, map, n_ctas, cluster, device, st);
+}
+
+// CTAs of a cluster for each head of each sequence, all at once on the GPU; 0: the line.  The line is even whatever the lengths, but lays
+// itself out and joins its heads in a second launch; a cluster does neither.  us a call in clusters / on the line, e4m3, 128 elements: 8 KV
+// heads of 1000 tokens 6.8 / 11.8, of 3064 8.2 / 10.4, of 15000 16.0 / 17.1, of 30000 26.3 / 23.4; int8, 64 heads of 1000 8.7 / 13.5, of 3000
+// 15.2 / 17.5, of 7500 29.3 / 26.4; 128 heads of 3000 24.5 / 25.9.  What a CTA may have to read decides: the table's width says how much.
+constexpr long long CLUSTER_BYTES = 512 << 10;
+int cluster_of(const AttendArgs &a, int d, int n_sm) {
+  const long long heads = (long long)a.bv.n_seqs * a.pv.H;
+  const int c = heads <= 16 ? 8 : heads <= 32 ? 4 : heads <= 64 ? 2 : heads <= n_sm ? 1 : 0;
+  return c && (long long)a.bv.stride * a.pv.T * 2 * d <= c * CLUSTER_BYTES ? c : 0;
 }
 
 wnw_status_t check_heads(const wnw_pages_t *p, int n_q_heads) {
@@ -694,17 +787,18 @@ extern "C" wnw_status_t wnw_pages_attend(const wnw_pages_attend_t *call) {
   if (((long long)batch->n_rows / a.rt + batch->n_seqs) * pages->n_kv_heads > 1ll << 30) return WNW_ERR_CAPACITY;
   const cudaStream_t st = (cudaStream_t)call->cuda_stream;
   cudaError_t e;
+  const int cluster = prompt ? 0 : cluster_of(a, d, n_sm), n_ctas = cluster ? cluster * a.bv.n_seqs * a.pv.H : n_sm;
   if (prompt) {
     e = launch_prompt(a, d, pages->format, n_sm, pages->device, st);
   } else {
     CUtensorMap map;
     memset(&map, 0, sizeof(map));
     if (pages->n_pages && !encode_map(&map, a.pv, d)) return WNW_ERR_CUDA;
-    if (d == 64) e = pages->format == WNW_PAGES_E4M3 ? launch<64, WNW_PAGES_E4M3>(a, map, nt, n_sm, pages->device, st) : launch<64, WNW_PAGES_INT8>(a, map, nt, n_sm, pages->device, st);
-    else e = pages->format == WNW_PAGES_E4M3 ? launch<128, WNW_PAGES_E4M3>(a, map, nt, n_sm, pages->device, st) : launch<128, WNW_PAGES_INT8>(a, map, nt, n_sm, pages->device, st);
+    if (d == 64) e = pages->format == WNW_PAGES_E4M3 ? launch<64, WNW_PAGES_E4M3>(a, map, nt, n_ctas, cluster, pages->device, st) : launch<64, WNW_PAGES_INT8>(a, map, nt, n_ctas, cluster, pages->device, st);
+    else e = pages->format == WNW_PAGES_E4M3 ? launch<128, WNW_PAGES_E4M3>(a, map, nt, n_ctas, cluster, pages->device, st) : launch<128, WNW_PAGES_INT8>(a, map, nt, n_ctas, cluster, pages->device, st);
   }
-  if (e != cudaSuccess) return WNW_ERR_CUDA;
+  if (e != cudaSuccess || cluster) return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
   const dim3 grid(n_sm, prompt ? 16 : a.rt * a.g);
-  e = pg_launch(d == 64 ? wnw_pages_join_kernel<64> : wnw_pages_join_kernel<128>, grid, 128, 0, st, a);
+  e = pg_launch(d == 64 ? wnw_pages_join_kernel<64> : wnw_pages_join_kernel<128>, grid, 128, 0, st, 0, a);
   return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
 }

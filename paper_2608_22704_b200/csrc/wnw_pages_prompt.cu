@@ -712,7 +712,7 @@ template <int D, int FMT> cudaError_t launch(const AttendArgs &a, int n_ctas, in
     if (e != cudaSuccess) return e;
     ready.fetch_or(1ull << device, std::memory_order_release);
   }
-  return pg_launch(wnw_pages_prompt_kernel<D, FMT>, dim3(n_ctas), PP_THREADS, smem_bytes<D>(), st, a);
+  return pg_launch(wnw_pages_prompt_kernel<D, FMT>, dim3(n_ctas), PP_THREADS, smem_bytes<D>(), st, 0, a);
 }
 
 }  // namespace

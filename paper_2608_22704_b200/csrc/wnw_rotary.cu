@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(ROT_THREADS) wnw_rotate_kernel(const __grid_co
 template <typename T> cudaError_t launch(const RotateArgs &a, bool vec, cudaStream_t st) {
   const int grid = (a.n_tokens + a.tokens_per_cta - 1) / a.tokens_per_cta;
   const size_t smem = sizeof(float2) * a.tokens_per_cta * a.rot.n_pairs;
-  return pg_launch(vec ? wnw_rotate_kernel<T, true> : wnw_rotate_kernel<T, false>, dim3(grid), ROT_THREADS, smem, st, a);
+  return pg_launch(vec ? wnw_rotate_kernel<T, true> : wnw_rotate_kernel<T, false>, dim3(grid), ROT_THREADS, smem, st, 0, a);
 }
 
 }  // namespace
