@@ -5,6 +5,7 @@
 // memory bounds them; a CTA takes one page of one KV head, K or V, whose scale it thereby owns: no atomics, one order of everything.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "wnw_pages.cuh"
 
@@ -44,6 +45,17 @@ template <int FMT> __device__ __forceinline__ int exponent_for(uint32_t bits) {
 }
 __device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
+// Magnitudes of 16-bit numbers as the bits of floats
+template <typename T> struct Bits;
+template <> struct Bits<__nv_bfloat16> {
+  static constexpr uint32_t INF = 0x7f80;
+  static __device__ __forceinline__ uint32_t as_float(uint32_t x) { return x << 16; }
+};
+template <> struct Bits<__half> {
+  static constexpr uint32_t INF = 0x7c00;
+  static __device__ __forceinline__ uint32_t as_float(uint32_t x) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)x))); }
+};
+
 // What of a sequence a call covers: tokens [first, end), rows from row0 on; everything inside the table and the tensors
 struct Span { int first, end, row0; };
 __device__ __forceinline__ Span span_of(const PagesView &pv, const BatchView &b, int s) {
@@ -69,105 +81,123 @@ struct WriteArgs {
   long long axis_stride;
 };
 
-// Elements that a thread takes at a time: 8 from `lo` on and 8 from `hi` on, so that the turn of a pair stays in the thread.
+// Keys that are turned: a thread takes 8 elements from `lo` on and 8 from `hi` on, so that the turn of a pair stays with it.
 template <int D> __device__ __forceinline__ void unit_offsets(int u, int n_pairs, int neighbours, int *lo, int *hi) {
   const int turned = n_pairs / 8;
   if (u < turned && !neighbours) { *lo = 8 * u; *hi = 8 * u + n_pairs; }
   else { *lo = 16 * u; *hi = 16 * u + 8; }             // also what lies behind the pairs: 2 * n_pairs + 16 * (u - turned)
 }
+// 16 elements of a row turned by its position; p0: the first of their eight pairs
+template <typename T> __device__ __forceinline__ void turn_unit(const WriteArgs &a, int row, int p0, uint4 &lo, uint4 &hi) {
+  uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  if (a.rot.neighbours) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const float2 c = pg_angle(a.rot, p0 + q, a.positions[a.rot.axis[p0 + q] * a.axis_stride + row]);
+      const float2 f = Pair<T>::get(w[q]), t = pg_turn(f.x, f.y, c);
+      w[q] = Pair<T>::put(t.x, t.y);
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float2 c = pg_angle(a.rot, p0 + 2 * q, a.positions[a.rot.axis[p0 + 2 * q] * a.axis_stride + row]);
+      const float2 d = pg_angle(a.rot, p0 + 2 * q + 1, a.positions[a.rot.axis[p0 + 2 * q + 1] * a.axis_stride + row]);
+      const float2 f = Pair<T>::get(w[q]), g = Pair<T>::get(w[4 + q]);
+      const float2 t = pg_turn(f.x, g.x, c), z = pg_turn(f.y, g.y, d);
+      w[q] = Pair<T>::put(t.x, z.x);
+      w[4 + q] = Pair<T>::put(t.y, z.y);
+    }
+  }
+  lo = make_uint4(w[0], w[1], w[2], w[3]);
+  hi = make_uint4(w[4], w[5], w[6], w[7]);
+}
 
-// CTA: (pages of a sequence, one at a time; KV head and K|V; sequence).  UN units of 16 elements a thread at most.
-template <typename T, int D, int FMT, int UN, int THREADS>
-__global__ void __launch_bounds__(THREADS) wnw_pages_write_kernel(const __grid_constant__ WriteArgs a) {
-  constexpr int UPR = D / 16;                          // units of a row
-  __shared__ uint32_t red[16];
+// CTA: (pages of a sequence, one at a time; KV head and K|V; sequence).  A thread keeps its N pieces of eight elements in registers from the
+// one pass over the rows to the codes.
+template <typename T, int D, int FMT, int N, int THREADS, bool TURN>
+__global__ void __launch_bounds__(THREADS, TURN ? 1 : 1024 / THREADS) wnw_pages_write_kernel(const __grid_constant__ WriteArgs a) {
+  constexpr int PPR = D / 8;                           // pieces of a row
+  __shared__ uint32_t red[THREADS / 32];
   const PagesView &pv = a.pv;
-  const int s = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1, nt = THREADS;
+  const int s = blockIdx.z, head = blockIdx.x >> 1, which = blockIdx.x & 1, tid = threadIdx.x;
   pg_let_next_start();
   pg_wait_for_stream();
   const Span sp = span_of(pv, a.bv, s);
   if (sp.first >= sp.end) return;
-  const bool turn = a.rot.n_pairs && which == 0;
   const int page0 = sp.first / pv.T, n_touched = (sp.end - 1) / pv.T - page0 + 1;
-  for (int i = blockIdx.x; i < n_touched; i += gridDim.x) {
-    const int base = (page0 + i) * pv.T, t0 = max(sp.first, base) - base, t1 = min(sp.end - base, pv.T);
+  // Piece j of the thread: row and element of the page's new rows.  Where keys are turned, pieces 2i and 2i + 1 are the two of a unit.
+  auto piece = [&](int j, int *r, int *e) {
+    if (TURN) {
+      const int u = tid + (j >> 1) * THREADS;
+      int lo, hi;
+      unit_offsets<D>(u % (PPR / 2), which ? 0 : a.rot.n_pairs, a.rot.neighbours, &lo, &hi);
+      *r = u / (PPR / 2);
+      *e = j & 1 ? hi : lo;
+    } else {
+      const int u = tid + j * THREADS;
+      *r = u / PPR;
+      *e = u % PPR * 8;
+    }
+  };
+  for (int i = blockIdx.y; i < n_touched; i += gridDim.y) {
+    const int base = (page0 + i) * pv.T, t0 = max(sp.first, base) - base, t1 = min(sp.end - base, pv.T), rows = t1 - t0;
     const int page = a.bv.table[(long long)s * a.bv.stride + page0 + i];
+    const int row0 = sp.row0 + base + t0 - sp.first;
+    const T *in = reinterpret_cast<const T *>(a.in[which].p) + (long long)row0 * a.in[which].row + head * a.in[which].head;
+    uint4 x[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      int r, e;
+      piece(j, &r, &e);
+      x[j] = r < rows ? *reinterpret_cast<const uint4 *>(in + r * a.in[which].row + e) : make_uint4(0, 0, 0, 0);
+    }
     if (page < 0 || page >= pv.n_pages) {
-      if (threadIdx.x == 0) pg_report(pv, WNW_PAGES_BAD_PAGE);
+      if (tid == 0) pg_report(pv, WNW_PAGES_BAD_PAGE);
       continue;
     }
     float *scale = pv.scales + page * pv.scale_stride + head * 2 + which;
     const float old_scale = t0 ? *scale : 0.f;         // needed late, asked for early
-    uint4 x[UN][2];
-    uint32_t most = 0;
-    const int n_units = (t1 - t0) * UPR;
+    if (TURN && which == 0) {
 #pragma unroll
-    for (int j = 0; j < UN; ++j) {
-      const int u = threadIdx.x + j * nt;
-      x[j][0] = x[j][1] = make_uint4(0, 0, 0, 0);
-      if (u < n_units) {
-        const int r = u / UPR;
-        int lo, hi;
-        unit_offsets<D>(u % UPR, turn ? a.rot.n_pairs : 0, a.rot.neighbours, &lo, &hi);
-        const T *p = reinterpret_cast<const T *>(a.in[which].p) + (long long)(sp.row0 + base + t0 + r - sp.first) * a.in[which].row + head * a.in[which].head;
-        x[j][0] = *reinterpret_cast<const uint4 *>(p + lo);
-        x[j][1] = *reinterpret_cast<const uint4 *>(p + hi);
+      for (int j = 0; j < N; j += 2) {
+        const int u = tid + (j >> 1) * THREADS, p0 = 8 * (u % (PPR / 2)), r = u / (PPR / 2);
+        if (r < rows && p0 < a.rot.n_pairs) turn_unit<T>(a, row0 + r, p0, x[j], x[j + 1]);
       }
     }
-    if (turn) {
+    // The largest magnitude: as integers, two at a time, while all are finite
+    uint32_t both = 0;
 #pragma unroll
-      for (int j = 0; j < UN; ++j) {
-        const int u = threadIdx.x + j * nt, p0 = 8 * (u % UPR);
-        if (u < n_units && p0 < a.rot.n_pairs) {
-          const int row = sp.row0 + base + t0 + u / UPR - sp.first;
-          uint32_t w[8] = {x[j][0].x, x[j][0].y, x[j][0].z, x[j][0].w, x[j][1].x, x[j][1].y, x[j][1].z, x[j][1].w};
-          if (a.rot.neighbours) {
+    for (int j = 0; j < N; ++j) {
+      both = __vmaxu2(both, __vmaxu2(__vmaxu2(x[j].x & 0x7fff7fffu, x[j].y & 0x7fff7fffu), __vmaxu2(x[j].z & 0x7fff7fffu, x[j].w & 0x7fff7fffu)));
+    }
+    const uint32_t top = max(both & 0xffffu, both >> 16);
+    const bool odd = top >= Bits<T>::INF;               // the thread's elements are not all finite
+    uint32_t most = Bits<T>::as_float(top);
+    if (odd) {
+      most = 0;
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-              const float2 c = pg_angle(a.rot, p0 + q, a.positions[a.rot.axis[p0 + q] * a.axis_stride + row]);
-              const float2 f = Pair<T>::get(w[q]);
-              const float2 t = pg_turn(f.x, f.y, c);
-              w[q] = Pair<T>::put(t.x, t.y);
-            }
-          } else {
+      for (int j = 0; j < N; ++j) {
+        const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const float2 c = pg_angle(a.rot, p0 + 2 * q, a.positions[a.rot.axis[p0 + 2 * q] * a.axis_stride + row]);
-              const float2 d = pg_angle(a.rot, p0 + 2 * q + 1, a.positions[a.rot.axis[p0 + 2 * q + 1] * a.axis_stride + row]);
-              const float2 f = Pair<T>::get(w[q]), g = Pair<T>::get(w[4 + q]);
-              const float2 t = pg_turn(f.x, g.x, c), z = pg_turn(f.y, g.y, d);
-              w[q] = Pair<T>::put(t.x, z.x);
-              w[4 + q] = Pair<T>::put(t.y, z.y);
-            }
-          }
-          x[j][0] = make_uint4(w[0], w[1], w[2], w[3]);
-          x[j][1] = make_uint4(w[4], w[5], w[6], w[7]);
+        for (int q = 0; q < 8; ++q) {
+          const uint32_t m = w[q >> 1] >> 16 * (q & 1) & 0x7fffu;
+          most = max(most, m < Bits<T>::INF ? Bits<T>::as_float(m) : 0u);
         }
       }
     }
-#pragma unroll
-    for (int j = 0; j < UN; ++j) {
-      const uint32_t w[8] = {x[j][0].x, x[j][0].y, x[j][0].z, x[j][0].w, x[j][1].x, x[j][1].y, x[j][1].z, x[j][1].w};
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const float2 f = Pair<T>::get(w[q]);
-        const uint32_t m = __float_as_uint(f.x) & 0x7fffffffu, n = __float_as_uint(f.y) & 0x7fffffffu;
-        most = max(most, m < 0x7f800000u ? m : 0u);
-        most = max(most, n < 0x7f800000u ? n : 0u);
-      }
-    }
     most = __reduce_max_sync(0xffffffffu, most);
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = most;
+    if ((tid & 31) == 0) red[tid >> 5] = most;
     __syncthreads();
-    for (int w = 0; w < nt / 32; ++w) most = max(most, red[w]);
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) most = max(most, red[w]);
     __syncthreads();                                   // red is free for the next page
-    int e = exponent_for<FMT>(most);
+    int e_new = exponent_for<FMT>(most);
     unsigned char *block = pv.codes + page * pv.page_stride + (long long)(head * 2 + which) * pv.T * D;
     if (t0) {
       const int had = max(PG_LOWEST, min(pg_highest(FMT), (int)(__float_as_uint(old_scale) >> 23 & 255) - 127));
-      if (e > had) {                                   // rows of before, for the raised scale
-        const float down = power(max(-64, had - e));   // (codes / 2^64 are 0 already)
-        for (int u = threadIdx.x; u < t0 * (D / 16); u += nt) {
+      if (e_new > had) {                               // rows of before, for the raised scale
+        const float down = power(max(-64, had - e_new));   // (codes / 2^64 are 0 already)
+        for (int u = tid; u < t0 * (D / 16); u += THREADS) {
           uint4 *p = reinterpret_cast<uint4 *>(block + (long long)u * 16), v = *p;
           uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -179,26 +209,29 @@ __global__ void __launch_bounds__(THREADS) wnw_pages_write_kernel(const __grid_c
           *p = make_uint4(w[0], w[1], w[2], w[3]);
         }
       }
-      e = max(e, had);
+      e_new = max(e_new, had);
     }
-    if (threadIdx.x == 0) *scale = power(e);
-    const float by = power(-e);
+    if (tid == 0) *scale = power(e_new);
+    const float by = power(-e_new);
+    const bool plain = !odd && e_new < pg_highest(FMT);   // no code beyond the largest
 #pragma unroll
-    for (int j = 0; j < UN; ++j) {
-      const int u = threadIdx.x + j * nt;
-      if (u < n_units) {
-        int lo, hi;
-        unit_offsets<D>(u % UPR, turn ? a.rot.n_pairs : 0, a.rot.neighbours, &lo, &hi);
-        unsigned char *p = block + (long long)(t0 + u / UPR) * D;
-        const uint32_t w[8] = {x[j][0].x, x[j][0].y, x[j][0].z, x[j][0].w, x[j][1].x, x[j][1].y, x[j][1].z, x[j][1].w};
-        uint32_t c[4];
+    for (int j = 0; j < N; ++j) {
+      int r, e;
+      piece(j, &r, &e);
+      if (r < rows) {
+        const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+        uint32_t c[2];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < 2; ++q) {
           const float2 f = Pair<T>::get(w[2 * q]), g = Pair<T>::get(w[2 * q + 1]);
-          c[q] = encode4<FMT>(f.x * by, f.y * by, g.x * by, g.y * by);
+          if (FMT == WNW_PAGES_INT8 && plain) {          // rounded where it is added to 1.5 * 2^23: the integer is the sum's low byte
+            const float u = __fmaf_rn(f.x, by, 12582912.f), v = __fmaf_rn(f.y, by, 12582912.f), y = __fmaf_rn(g.x, by, 12582912.f), z = __fmaf_rn(g.y, by, 12582912.f);
+            c[q] = __byte_perm(__byte_perm(__float_as_uint(u), __float_as_uint(v), 0x0040), __byte_perm(__float_as_uint(y), __float_as_uint(z), 0x0040), 0x5410);
+          } else {
+            c[q] = encode4<FMT>(f.x * by, f.y * by, g.x * by, g.y * by);
+          }
         }
-        *reinterpret_cast<uint2 *>(p + lo) = make_uint2(c[0], c[1]);
-        *reinterpret_cast<uint2 *>(p + hi) = make_uint2(c[2], c[3]);
+        *reinterpret_cast<uint2 *>(block + (t0 + r) * D + e) = make_uint2(c[0], c[1]);
       }
     }
   }
@@ -212,42 +245,47 @@ struct ReadArgs {
 };
 
 template <typename T, int D, int FMT>
-__global__ void __launch_bounds__(256) wnw_pages_read_kernel(const __grid_constant__ ReadArgs a) {
-  constexpr int UPR = D / 16;
+__global__ void __launch_bounds__(256, 8) wnw_pages_read_kernel(const __grid_constant__ ReadArgs a) {
+  constexpr int PPR = D / 8, N = 4;                    // pieces of eight codes of a row; of a thread in flight
   const PagesView &pv = a.pv;
-  const int s = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1, nt = 256;
+  const int s = blockIdx.z, head = blockIdx.x >> 1, which = blockIdx.x & 1;
   pg_let_next_start();
   pg_wait_for_stream();
   const Span sp = span_of(pv, a.bv, s);
   if (sp.first >= sp.end) return;
   const int page0 = sp.first / pv.T, n_touched = (sp.end - 1) / pv.T - page0 + 1;
-  for (int i = blockIdx.x; i < n_touched; i += gridDim.x) {
+  for (int i = blockIdx.y; i < n_touched; i += gridDim.y) {
     const int base = (page0 + i) * pv.T, t0 = max(sp.first, base) - base, t1 = min(sp.end - base, pv.T);
     const int page = a.bv.table[(long long)s * a.bv.stride + page0 + i];
     const bool there = page >= 0 && page < pv.n_pages;
     if (!there && threadIdx.x == 0) pg_report(pv, WNW_PAGES_BAD_PAGE);
     const float scale = there ? pv.scales[page * pv.scale_stride + head * 2 + which] : 0.f;
-    const unsigned char *block = pv.codes + (there ? page : 0) * pv.page_stride + (long long)(head * 2 + which) * pv.T * D;
-    for (int u = threadIdx.x; u < (t1 - t0) * UPR; u += nt) {
-      const int r = u / UPR, c = u % UPR;
-      const uint4 v = there ? *reinterpret_cast<const uint4 *>(block + (long long)(t0 + r) * D + 16 * c) : make_uint4(0, 0, 0, 0);
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-      uint32_t o[8];
+    const unsigned char *block = pv.codes + (there ? page : 0) * pv.page_stride + ((long long)(head * 2 + which) * pv.T + t0) * D;
+    T *out = reinterpret_cast<T *>(a.out[which].p) + (long long)(sp.row0 + base + t0 - sp.first) * a.out[which].row + head * a.out[which].head;
+    const int all = (t1 - t0) * PPR;
+    for (int u0 = threadIdx.x; u0 < all; u0 += 256 * N) {
+      uint2 v[N];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float f[4];
-        decode4<FMT>(w[q], f);
-#pragma unroll
-        for (int z = 0; z < 4; ++z) {
-          f[z] *= scale;
-          if (sizeof(T) == 2 && std::is_same<T, __half>::value && fabsf(f[z]) > 65504.f) f[z] = copysignf(65504.f, f[z]);
-        }
-        o[2 * q] = Pair<T>::put(f[0], f[1]);
-        o[2 * q + 1] = Pair<T>::put(f[2], f[3]);
+      for (int k = 0; k < N; ++k) {
+        const int u = u0 + 256 * k;
+        v[k] = there && u < all ? *reinterpret_cast<const uint2 *>(block + u * 8) : make_uint2(0, 0);
       }
-      T *p = reinterpret_cast<T *>(a.out[which].p) + (long long)(sp.row0 + base + t0 + r - sp.first) * a.out[which].row + head * a.out[which].head + 16 * c;
-      reinterpret_cast<uint4 *>(p)[0] = make_uint4(o[0], o[1], o[2], o[3]);
-      reinterpret_cast<uint4 *>(p)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const int u = u0 + 256 * k;
+        if (u < all) {
+          float f[8];
+          decode4<FMT>(v[k].x, reinterpret_cast<float (&)[4]>(f[0]));
+          decode4<FMT>(v[k].y, reinterpret_cast<float (&)[4]>(f[4]));
+#pragma unroll
+          for (int z = 0; z < 8; ++z) {
+            f[z] *= scale;
+            if (std::is_same<T, __half>::value && fabsf(f[z]) > 65504.f) f[z] = copysignf(65504.f, f[z]);
+          }
+          *reinterpret_cast<uint4 *>(out + (long long)(u / PPR) * a.out[which].row + u % PPR * 8) =
+              make_uint4(Pair<T>::put(f[0], f[1]), Pair<T>::put(f[2], f[3]), Pair<T>::put(f[4], f[5]), Pair<T>::put(f[6], f[7]));
+        }
+      }
     }
   }
 }
@@ -255,14 +293,18 @@ __global__ void __launch_bounds__(256) wnw_pages_read_kernel(const __grid_consta
 // Pages that a sequence's rows can touch, by what the caller says of the rows; the kernels' loops cover the rest.
 int pages_touched(const wnw_batch_t &b, int T) {
   const int rows = b.max_rows > 0 ? std::min(b.max_rows, b.n_rows) : b.n_rows;
-  return std::min((rows + T - 2) / T + 1, 65536);
+  return std::min((rows + T - 2) / T + 1, 65535);
 }
 
+template <typename T, int D, int FMT, bool TURN> cudaError_t launch_write(const WriteArgs &a, dim3 grid, cudaStream_t st) {
+  const int pieces = a.pv.T * (D / 8);
+  if (pieces <= 512) return pg_launch(wnw_pages_write_kernel<T, D, FMT, 4, 128, TURN>, grid, 128, 0, st, 0, a);
+  if (pieces <= 1024) return pg_launch(wnw_pages_write_kernel<T, D, FMT, 4, 256, TURN>, grid, 256, 0, st, 0, a);
+  if (pieces <= 2048) return pg_launch(wnw_pages_write_kernel<T, D, FMT, 8, 256, TURN>, grid, 256, 0, st, 0, a);
+  return pg_launch(wnw_pages_write_kernel<T, D, FMT, 8, 512, TURN>, grid, 512, 0, st, 0, a);
+}
 template <typename T, int D, int FMT> cudaError_t launch_write(const WriteArgs &a, dim3 grid, cudaStream_t st) {
-  const int units = a.pv.T * (D / 16);
-  if (units <= 512) return pg_launch(wnw_pages_write_kernel<T, D, FMT, 2, 256>, grid, 256, 0, st, 0, a);
-  if (units <= 1024) return pg_launch(wnw_pages_write_kernel<T, D, FMT, 4, 256>, grid, 256, 0, st, 0, a);
-  return pg_launch(wnw_pages_write_kernel<T, D, FMT, 4, 512>, grid, 512, 0, st, 0, a);
+  return a.rot.n_pairs ? launch_write<T, D, FMT, true>(a, grid, st) : launch_write<T, D, FMT, false>(a, grid, st);
 }
 template <typename T> cudaError_t launch_write(const WriteArgs &a, int d, int fmt, dim3 grid, cudaStream_t st) {
   if (d == 64) return fmt == WNW_PAGES_E4M3 ? launch_write<T, 64, WNW_PAGES_E4M3>(a, grid, st) : launch_write<T, 64, WNW_PAGES_INT8>(a, grid, st);
@@ -345,7 +387,7 @@ extern "C" wnw_status_t wnw_pages_write(const wnw_pages_rows_t *call) {
   if (!call->batch.n_seqs || !call->batch.n_rows) return WNW_OK;
   OnDevice on(call->pages->device);
   if (!on.ok) return WNW_ERR_CUDA;
-  const dim3 grid(pages_touched(call->batch, a.pv.T), 2 * a.pv.H, call->batch.n_seqs);
+  const dim3 grid(2 * a.pv.H, pages_touched(call->batch, a.pv.T), call->batch.n_seqs);   // (a token's heads lie beside one another)
   const cudaStream_t st = (cudaStream_t)call->cuda_stream;
   const int d = call->pages->head_dim, fmt = call->pages->format;
   const cudaError_t e = call->dtype == WNW_DTYPE_BF16 ? launch_write<__nv_bfloat16>(a, d, fmt, grid, st) : launch_write<__half>(a, d, fmt, grid, st);
@@ -362,7 +404,7 @@ extern "C" wnw_status_t wnw_pages_read(const wnw_pages_rows_t *call) {
   if (!call->batch.n_seqs || !call->batch.n_rows) return WNW_OK;
   OnDevice on(call->pages->device);
   if (!on.ok) return WNW_ERR_CUDA;
-  const dim3 grid(pages_touched(call->batch, a.pv.T), 2 * a.pv.H, call->batch.n_seqs);
+  const dim3 grid(2 * a.pv.H, pages_touched(call->batch, a.pv.T), call->batch.n_seqs);   // (a token's heads lie beside one another)
   const cudaStream_t st = (cudaStream_t)call->cuda_stream;
   const int d = call->pages->head_dim, fmt = call->pages->format;
   const cudaError_t e = call->dtype == WNW_DTYPE_BF16 ? launch_read<__nv_bfloat16>(a, d, fmt, grid, st) : launch_read<__half>(a, d, fmt, grid, st);

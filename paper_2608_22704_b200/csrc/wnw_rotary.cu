@@ -12,7 +12,7 @@
 namespace wnw {
 namespace {
 
-constexpr int ROT_THREADS = 256;
+constexpr int ROT_THREADS = 256, ROT_HEADS = 4;
 
 struct RotateArgs {
   RotaryView rot;
@@ -57,51 +57,82 @@ template <> struct Vec<float> {
   __device__ __forceinline__ uint4 put() const { return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])); }
 };
 
-// A unit of work is N pairs of one head and token: two vectors of 16 bytes (VEC), or one pair.
+// A unit of work is N pairs of one token in up to U heads, 16 bytes (VEC) or one element each of the pairs' two halves: the angles are
+// read once for the U heads, whose elements are on their way together.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(ROT_THREADS) wnw_rotate_kernel(const __grid_constant__ RotateArgs a) {
-  extern __shared__ float2 cs[];                        // [tokens_per_cta][n_pairs]
+__global__ void __launch_bounds__(ROT_THREADS, 3) wnw_rotate_kernel(const __grid_constant__ RotateArgs a) {
+  constexpr int N = VEC ? Vec<T>::N : 1, U = ROT_HEADS;
+  extern __shared__ __align__(16) float2 cs[];          // [tokens_per_cta][N / 2][units][2], without bank conflicts; N = 1: [token][pair]
   pg_let_next_start();
   pg_wait_for_stream();
-  const int np = a.rot.n_pairs, t0 = blockIdx.x * a.tokens_per_cta, nt = min(a.tokens_per_cta, a.n_tokens - t0);
+  const int np = a.rot.n_pairs, units = np / N, t0 = blockIdx.x * a.tokens_per_cta, nt = min(a.tokens_per_cta, a.n_tokens - t0);
   for (int i = threadIdx.x; i < nt * np; i += ROT_THREADS) {
     const int t = i / np, p = i - t * np;
-    cs[i] = pg_angle(a.rot, p, a.positions[a.rot.axis[p] * a.axis_stride + t0 + t]);
+    const float2 c = pg_angle(a.rot, p, a.positions[a.rot.axis[p] * a.axis_stride + t0 + t]);
+    cs[t * np + (VEC ? ((p % N >> 1) * units + p / N) * 2 + (p & 1) : p)] = c;
   }
-  __syncthreads();
-  constexpr int N = VEC ? Vec<T>::N : 1;
-  const int units = np / N, heads = a.n_heads[0] + a.n_heads[1], all = nt * heads * units;
-  for (int i = threadIdx.x; i < all; i += ROT_THREADS) {
-    const int row = i / units, u = i - row * units, t = row / heads, h0 = row - t * heads;
-    const int which = h0 >= a.n_heads[0], h = h0 - (which ? a.n_heads[0] : 0);
-    const T *in = reinterpret_cast<const T *>(a.in[which].p) + (t0 + t) * a.in[which].row + h * a.in[which].head;
-    T *out = reinterpret_cast<T *>(a.out[which].p) + (t0 + t) * a.out[which].row + h * a.out[which].head;
-    const float2 *c = cs + t * np + u * N;
-    const int lo = a.rot.neighbours ? 2 * N * u : N * u, hi = a.rot.neighbours ? lo + N : N * u + np;
-    if constexpr (VEC) {
-      Vec<T> x, y;
-      x.get(*reinterpret_cast<const uint4 *>(in + lo));
-      y.get(*reinterpret_cast<const uint4 *>(in + hi));
-      if (a.rot.neighbours) {
+  const int heads = a.n_heads[0] + a.n_heads[1], blocks = (heads + U - 1) / U, all = nt * blocks * units;
+  const bool nb = a.rot.neighbours;
+  const int up = nb ? N : np;                           // from a unit's first half to its second
+  bool ready = false;
+  for (int i = threadIdx.x; i < all || !ready; i += ROT_THREADS) {
+    const int row = i / units, u = i - row * units, t = row / blocks, h0 = (row - t * blocks) * U, n = i < all ? min(U, heads - h0) : 0;
+    const T *in[U];
+    T *out[U];
+    uint4 x[U], y[U];
 #pragma unroll
-        for (int j = 0; j < N / 2; ++j) {
-          const float2 s = pg_turn(x.x[2 * j], x.x[2 * j + 1], c[j]), t = pg_turn(y.x[2 * j], y.x[2 * j + 1], c[N / 2 + j]);
-          x.x[2 * j] = s.x; x.x[2 * j + 1] = s.y;
-          y.x[2 * j] = t.x; y.x[2 * j + 1] = t.y;
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const float2 s = pg_turn(x.x[j], y.x[j], c[j]);
-          x.x[j] = s.x; y.x[j] = s.y;
+    for (int k = 0; k < U; ++k)
+      if (k < n) {
+        const int which = h0 + k >= a.n_heads[0], h = h0 + k - (which ? a.n_heads[0] : 0), lo = (nb ? 2 : 1) * N * u;
+        in[k] = reinterpret_cast<const T *>(a.in[which].p) + (long long)(t0 + t) * a.in[which].row + h * a.in[which].head + lo;
+        out[k] = reinterpret_cast<T *>(a.out[which].p) + (long long)(t0 + t) * a.out[which].row + h * a.out[which].head + lo;
+        if constexpr (VEC) {
+          x[k] = *reinterpret_cast<const uint4 *>(in[k]);
+          y[k] = *reinterpret_cast<const uint4 *>(in[k] + up);
         }
       }
-      *reinterpret_cast<uint4 *>(out + lo) = x.put();
-      *reinterpret_cast<uint4 *>(out + hi) = y.put();
+    if (!ready) __syncthreads();                        // (the angles, while the first elements are on their way)
+    ready = true;
+    if (!n) continue;
+    float2 c[N];
+    if constexpr (VEC) {
+#pragma unroll
+      for (int j = 0; j < N; j += 2) {
+        const float4 e = *reinterpret_cast<const float4 *>(cs + t * np + ((j >> 1) * units + u) * 2);
+        c[j] = make_float2(e.x, e.y);
+        c[j + 1] = make_float2(e.z, e.w);
+      }
     } else {
-      const float2 s = pg_turn(Elems<T>::get(in + lo), Elems<T>::get(in + hi), c[0]);
-      Elems<T>::put(out + lo, s.x);
-      Elems<T>::put(out + hi, s.y);
+      c[0] = cs[t * np + u];
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (k >= n) break;
+      if constexpr (VEC) {
+        Vec<T> p, q;
+        p.get(x[k]);
+        q.get(y[k]);
+        if (nb) {
+#pragma unroll
+          for (int j = 0; j < N / 2; ++j) {
+            const float2 s = pg_turn(p.x[2 * j], p.x[2 * j + 1], c[j]), z = pg_turn(q.x[2 * j], q.x[2 * j + 1], c[N / 2 + j]);
+            p.x[2 * j] = s.x; p.x[2 * j + 1] = s.y;
+            q.x[2 * j] = z.x; q.x[2 * j + 1] = z.y;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < N; ++j) {
+            const float2 s = pg_turn(p.x[j], q.x[j], c[j]);
+            p.x[j] = s.x; q.x[j] = s.y;
+          }
+        }
+        *reinterpret_cast<uint4 *>(out[k]) = p.put();
+        *reinterpret_cast<uint4 *>(out[k] + up) = q.put();
+      } else {
+        const float2 s = pg_turn(Elems<T>::get(in[k]), Elems<T>::get(in[k] + up), c[0]);
+        Elems<T>::put(out[k], s.x);
+        Elems<T>::put(out[k] + up, s.y);
+      }
     }
   }
   if (a.tail) {                                          // what the pairs leave, where the output is another tensor
@@ -201,7 +232,7 @@ extern "C" wnw_status_t wnw_rotate(const wnw_rotate_t *call) {
   OnDevice on(call->device);
   int n_sm = 0;
   if (!on.ok || pg_sms(call->device, &n_sm) != WNW_OK) return WNW_ERR_CUDA;
-  a.tokens_per_cta = std::max(1, std::min(16, n_tokens / (n_sm * 8)));
+  a.tokens_per_cta = std::max(1, std::min(16, n_tokens / (n_sm * 4)));
   const cudaStream_t st = (cudaStream_t)call->cuda_stream;
   const cudaError_t e = dtype == WNW_DTYPE_BF16 ? launch<__nv_bfloat16>(a, vec, st) : dtype == WNW_DTYPE_FP16 ? launch<__half>(a, vec, st)
                                                                                                               : launch<float>(a, vec, st);
