@@ -88,20 +88,22 @@ template <int D> __device__ __forceinline__ void unit_offsets(int u, int n_pairs
   else { *lo = 16 * u; *hi = 16 * u + 8; }             // also what lies behind the pairs: 2 * n_pairs + 16 * (u - turned)
 }
 // 16 elements of a row turned by its position; p0: the first of their eight pairs
-template <typename T> __device__ __forceinline__ void turn_unit(const WriteArgs &a, int row, int p0, uint4 &lo, uint4 &hi) {
+struct Plan { double turns[128]; int axis[128]; };     // in shared memory: lanes want different pairs
+template <typename T> __device__ __forceinline__ void turn_unit(const WriteArgs &a, const Plan &plan, int row, int p0, uint4 &lo, uint4 &hi) {
+  auto angle = [&](int p) { return pg_angle(plan.turns[p], a.positions[plan.axis[p] * a.axis_stride + row]); };
   uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
   if (a.rot.neighbours) {
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-      const float2 c = pg_angle(a.rot, p0 + q, a.positions[a.rot.axis[p0 + q] * a.axis_stride + row]);
+      const float2 c = angle(p0 + q);
       const float2 f = Pair<T>::get(w[q]), t = pg_turn(f.x, f.y, c);
       w[q] = Pair<T>::put(t.x, t.y);
     }
   } else {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const float2 c = pg_angle(a.rot, p0 + 2 * q, a.positions[a.rot.axis[p0 + 2 * q] * a.axis_stride + row]);
-      const float2 d = pg_angle(a.rot, p0 + 2 * q + 1, a.positions[a.rot.axis[p0 + 2 * q + 1] * a.axis_stride + row]);
+      const float2 c = angle(p0 + 2 * q);
+      const float2 d = angle(p0 + 2 * q + 1);
       const float2 f = Pair<T>::get(w[q]), g = Pair<T>::get(w[4 + q]);
       const float2 t = pg_turn(f.x, g.x, c), z = pg_turn(f.y, g.y, d);
       w[q] = Pair<T>::put(t.x, z.x);
@@ -124,6 +126,11 @@ __global__ void __launch_bounds__(THREADS, TURN ? 1 : 1024 / THREADS) wnw_pages_
   pg_wait_for_stream();
   const Span sp = span_of(pv, a.bv, s);
   if (sp.first >= sp.end) return;
+  __shared__ Plan plan;
+  if (TURN && which == 0) {
+    for (int p = tid; p < a.rot.n_pairs; p += THREADS) { plan.turns[p] = a.rot.turns[p]; plan.axis[p] = a.rot.axis[p]; }
+    __syncthreads();
+  }
   const int page0 = sp.first / pv.T, n_touched = (sp.end - 1) / pv.T - page0 + 1;
   // Piece j of the thread: row and element of the page's new rows.  Where keys are turned, pieces 2i and 2i + 1 are the two of a unit.
   auto piece = [&](int j, int *r, int *e) {
@@ -161,7 +168,7 @@ __global__ void __launch_bounds__(THREADS, TURN ? 1 : 1024 / THREADS) wnw_pages_
 #pragma unroll
       for (int j = 0; j < N; j += 2) {
         const int u = tid + (j >> 1) * THREADS, p0 = 8 * (u % (PPR / 2)), r = u / (PPR / 2);
-        if (r < rows && p0 < a.rot.n_pairs) turn_unit<T>(a, row0 + r, p0, x[j], x[j + 1]);
+        if (r < rows && p0 < a.rot.n_pairs) turn_unit<T>(a, plan, row0 + r, p0, x[j], x[j + 1]);
       }
     }
     // The largest magnitude: as integers, two at a time, while all are finite

@@ -46,12 +46,11 @@ __device__ __forceinline__ void pg_report(const PagesView &pv, int bit) {
 
 // cos and sin of positions * frequency.  64 bits hold position x turns to 2^-22 of a turn at the farthest int32 position; what is left
 // after whole turns is taken in 32.
-__device__ __forceinline__ float2 pg_angle(const RotaryView &r, int pair, int position) {
-  double t = (double)position * r.turns[pair];
+__device__ __forceinline__ float2 pg_angle(double turns, int position) {
+  double t = (double)position * turns;
   t -= rint(t);
   float2 cs;
   sincospif(2.f * (float)t, &cs.y, &cs.x);
-  cs.y *= r.sign;
   return cs;
 }
 
