@@ -712,12 +712,13 @@ template <int D, int FMT> cudaError_t launch(const AttendArgs &a, const CUtensor
 // CTAs of a cluster for each head of each sequence, all at once on the GPU; 0: the line.  The line is even whatever the lengths, but lays
 // itself out and joins its heads in a second launch; a cluster does neither.  us a call in clusters / on the line, e4m3, 128 elements: 8 KV
 // heads of 1000 tokens 6.8 / 11.8, of 3064 8.2 / 10.4, of 15000 16.0 / 17.1, of 30000 26.3 / 23.4; int8, 64 heads of 1000 8.7 / 13.5, of 3000
-// 15.2 / 17.5, of 7500 29.3 / 26.4; 128 heads of 3000 24.5 / 25.9.  What a CTA may have to read decides: the table's width says how much.
+// 15.2 / 17.5, of 7500 29.3 / 26.4; 128 heads of 3000 24.5 / 25.9.  What a CTA may have to read decides: the table's width says how much, and
+// the tiles of query tokens how often.
 constexpr long long CLUSTER_BYTES = 512 << 10;
-int cluster_of(const AttendArgs &a, int d, int n_sm) {
+int cluster_of(const AttendArgs &a, int tiles, int d, int n_sm) {
   const long long heads = (long long)a.bv.n_seqs * a.pv.H;
   const int c = heads <= 16 ? 8 : heads <= 32 ? 4 : heads <= 64 ? 2 : heads <= n_sm ? 1 : 0;
-  return c && (long long)a.bv.stride * a.pv.T * 2 * d <= c * CLUSTER_BYTES ? c : 0;
+  return c && (long long)a.bv.stride * a.pv.T * 2 * d * tiles <= c * CLUSTER_BYTES ? c : 0;
 }
 
 wnw_status_t check_heads(const wnw_pages_t *p, int n_q_heads) {
@@ -778,7 +779,10 @@ extern "C" wnw_status_t wnw_pages_attend(const wnw_pages_attend_t *call) {
   a.part_row = (PartRow *)((char *)workspace_dev + rows_at);
   a.part_head = (PartHead *)((char *)workspace_dev + heads_at);
   const int max_rows = batch->max_rows > 0 ? std::min(batch->max_rows, batch->n_rows) : batch->n_rows, d = pages->head_dim;
-  const bool prompt = (long long)max_rows * a.g > 16;
+  // Rows of a KV head that one call of a sequence brings: up to 16 in a pass over the codes, more in passes (the second from L2), from 49 on
+  // by the tensor cores' tiles of 128.  us, passes / tiles: 32 sequences of 7500 tokens, 8 KV heads of 128, int8, 20 rows 139 / 264, 32 rows
+  // 172 / 265, 48 rows 252 / 270, 64 rows 272 / 272; one of 3064, e4m3, 32 rows 20.7 / 26.4, 48 rows 30.5 / 28.3, 64 rows 40 / 30.
+  const bool prompt = (long long)max_rows * a.g > 48;
   const int nt = (long long)max_rows * a.g <= 8 ? 1 : 2;
   a.blocks = prompt ? PP_BLOCKS : 1;
   a.rb = prompt ? PP_ROWS : PA_ROWS;
@@ -787,7 +791,7 @@ extern "C" wnw_status_t wnw_pages_attend(const wnw_pages_attend_t *call) {
   if (((long long)batch->n_rows / a.rt + batch->n_seqs) * pages->n_kv_heads > 1ll << 30) return WNW_ERR_CAPACITY;
   const cudaStream_t st = (cudaStream_t)call->cuda_stream;
   cudaError_t e;
-  const int cluster = prompt ? 0 : cluster_of(a, d, n_sm), n_ctas = cluster ? cluster * a.bv.n_seqs * a.pv.H : n_sm;
+  const int cluster = prompt ? 0 : cluster_of(a, (max_rows + a.rt - 1) / a.rt, d, n_sm), n_ctas = cluster ? cluster * a.bv.n_seqs * a.pv.H : n_sm;
   if (prompt) {
     e = launch_prompt(a, d, pages->format, n_sm, pages->device, st);
   } else {
