@@ -38,6 +38,7 @@ struct Seg {
   int g0, n, y0;                     // first granule, granules, place of the first on the CTA's line
   int need;                          // granules from the head's first on that some row sees
   int len, row0, nq;                 // tokens of the sequence; first query row and query tokens of the tile
+  int r0, n_seq;                     // first query row and query tokens of the sequence
   int end0;                          // tokens that the tile's first query row sees; the next rows see one more each if causal
   int slot, n_parts;                 // slot -1: the whole head; else where the partial result goes
 };
@@ -134,8 +135,10 @@ __device__ __forceinline__ long long lay_out(const AttendArgs &a, long long *gra
   }
   return gbase;
 }
-// Granules that a CTA takes: equal stretches, none shorter than a granule for each warp.
-template <int W> __device__ __forceinline__ long long stretch(long long total, int n_ctas) { return max((long long)W, quotient(total + n_ctas - 1, n_ctas)); }
+// Granules that a CTA takes: equal stretches, none shorter than a granule for each warp or than a head.
+template <int W> __device__ __forceinline__ long long stretch(long long total, int n_items, int n_ctas) {
+  return max(n_items ? min((long long)W, quotient(total, n_items)) : 1, quotient(total + n_ctas - 1, n_ctas));
+}
 
 // CLUSTER: no line; cluster i takes KV head i % H of sequence i / H, its CTAs equal shares of the tokens, and their results meet in the
 // cluster's shared memory instead of in the workspace.
@@ -174,10 +177,11 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
     asm("mov.u32 %0, %%cluster_nctarank;\n" : "=r"(n_ranks));
   } else {
     const long long total = lay_out<W>(a, grans, items);
-    len_line = stretch<W>(total, gridDim.x);
+    n_items = items[a.bv.n_seqs];
+    len_line = stretch<W>(total, n_items, gridDim.x);
     x0 = min(total, blockIdx.x * len_line);
     x1 = min(total, x0 + len_line);
-    if (tid == 0) a.part_head[blockIdx.x] = PartHead{0, 0, 0, 0};
+    if (tid == 0) a.part_head[blockIdx.x] = PartHead{};
     if (x0 >= x1) return;
     // the first head of the line
     int lo = 0, hi = a.bv.n_seqs;                       // the last sequence that begins at or before x0 and is not empty
@@ -185,7 +189,6 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
     const int n_it = items[lo + 1] - items[lo];
     const long long per = quotient(grans[lo + 1] - grans[lo], n_it);
     item0 = items[lo] + (int)quotient(x0 - grans[lo], per);
-    n_items = items[a.bv.n_seqs];
   }
   // a lane's 16-byte pieces of K row r and V rows 2c, 2c + 1 (and 8 rows on) in a swizzled granule
   int k_at[G::KC], v_at[2];
@@ -211,6 +214,7 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
         Seg &sg = segs[0];
         sg.s = seq; sg.h = blockIdx.x / n_ranks % pv.H; sg.tile = item0;
         sg.len = len;
+        sg.r0 = r0; sg.n_seq = n;
         sg.nq = min(a.rt, n - first);
         sg.row0 = r0 + first;
         sg.end0 = a.causal ? len - n + first + 1 : len;
@@ -233,23 +237,25 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
           const int item = item0 + tid;
           int lo = 0, hi = a.bv.n_seqs;
           while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (items[mid] <= item) lo = mid; else hi = mid; }
-          const int n_it = items[lo + 1] - items[lo], it = item - items[lo], tiles = n_it / pv.H;
-          const long long per = quotient(grans[lo + 1] - grans[lo], n_it), b = grans[lo] + it * per, e = b + per;
+            const int cap = a.bv.stride * pv.T, r0 = max(a.bv.starts[lo], 0), n = max(0, min(a.bv.starts[lo + 1], a.bv.n_rows) - r0);
+          const int len = max(0, min(a.bv.lengths[lo], cap)), tiles = n <= a.rt ? 1 : (n + a.rt - 1) / a.rt, it = item - items[lo];
+          const int per = max(1, (len + PG_GR - 1) / PG_GR);
+          const long long b = grans[lo] + (long long)it * per, e = b + per;
           if (b < x1) {
             mine = 1;
             Seg &sg = segs[tid];
             const long long f = max(b, x0), l = min(e, x1);
-            sg.s = lo; sg.h = it / tiles; sg.tile = it % tiles;
+            sg.s = lo; sg.h = tiles == 1 ? it : it / tiles; sg.tile = tiles == 1 ? 0 : it % tiles;
             sg.g0 = (int)(f - b); sg.n = (int)(l - f); sg.y0 = (int)(f - x0);
-            const int cap = a.bv.stride * pv.T, r0 = max(a.bv.starts[lo], 0), r1 = min(a.bv.starts[lo + 1], a.bv.n_rows);
-            sg.len = max(0, min(a.bv.lengths[lo], cap));
-            sg.nq = min(a.rt, r1 - r0 - sg.tile * a.rt);
+            sg.len = len;
+            sg.r0 = r0; sg.n_seq = n;
+            sg.nq = min(a.rt, n - sg.tile * a.rt);
             sg.row0 = r0 + sg.tile * a.rt;
-            sg.end0 = a.causal ? sg.len - (r1 - r0) + sg.tile * a.rt + 1 : sg.len;
-            const int last = min(sg.len, a.causal ? sg.end0 + sg.nq - 1 : sg.len);
+            sg.end0 = a.causal ? len - n + sg.tile * a.rt + 1 : len;
+            const int last = min(len, a.causal ? sg.end0 + sg.nq - 1 : len);
             sg.need = last > 0 ? (last + PG_GR - 1) / PG_GR : 0;
             sg.slot = b >= x0 && e <= x1 ? -1 : b < x0 ? 0 : 1;
-            sg.n_parts = (int)(quotient(e - 1, len_line) - quotient(b, len_line) + 1);
+            sg.n_parts = sg.slot == 1 ? (int)quotient(e - 1 - x0, len_line) + 1 : 0;
           }
         }
         n_seg = __syncthreads_count(mine);
@@ -298,36 +304,44 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
         if (++p_stage == S) p_stage = 0;
       }
     };
+    // ---- the query rows: lane (r, c) holds row r of each tile of eight, the head_dim elements of its K bytes; asked for ahead ----
+    uint4 raw[NT][G::KC * 2];
+    auto ask_rows = [&](int si) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int k = 0; k < G::KC * 2; ++k) raw[t][k] = make_uint4(0, 0, 0, 0);
+        if (si < n_seg) {
+          const Seg &sg = segs[si];
+          const int j = t * 8 + r, tok = j / a.g, hd = j - tok * a.g;
+          if (j < a.rt * a.g && tok < sg.nq) {
+            const unsigned char *p = a.q.p + 2 * ((long long)(sg.row0 + tok) * a.q.row + (sg.h * a.g + hd) * a.q.head);
+#pragma unroll
+            for (int k = 0; k < G::KC; ++k) {
+              raw[t][2 * k] = *reinterpret_cast<const uint4 *>(p + 2 * (64 * k + 16 * c));
+              raw[t][2 * k + 1] = *reinterpret_cast<const uint4 *>(p + 2 * (64 * k + 16 * c) + 16);
+            }
+          }
+        }
+      }
+    };
+    ask_rows(0);
 #pragma unroll
     for (int k = 0; k < S - 1; ++k) fetch();
 
     int stage = 0;
     for (int si = 0; si < n_seg; ++si) {
       const Seg sg = segs[si];
-      // ---- the query rows: lane (r, c) holds row r of each tile of eight, the head_dim elements of its K bytes ----
       uint32_t qf[NT][G::KC * 8];
       float f_col[NT][2];                               // log2 scale of the scores' two columns 2c, 2c + 1
       int end_col[NT][2];                               // tokens that those rows see
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const int j = t * 8 + r, tok = j / a.g, hd = j - tok * a.g;
-        const bool real = j < a.rt * a.g && tok < sg.nq;
-        uint4 raw[G::KC * 2];
-#pragma unroll
-        for (int k = 0; k < G::KC * 2; ++k) raw[k] = make_uint4(0, 0, 0, 0);
-        if (real) {
-          const unsigned char *p = a.q.p + 2 * ((long long)(sg.row0 + tok) * a.q.row + (sg.h * a.g + hd) * a.q.head);
-#pragma unroll
-          for (int k = 0; k < G::KC; ++k) {
-            raw[2 * k] = *reinterpret_cast<const uint4 *>(p + 2 * (64 * k + 16 * c));
-            raw[2 * k + 1] = *reinterpret_cast<const uint4 *>(p + 2 * (64 * k + 16 * c) + 16);
-          }
-        }
         float most = 0.f;
         float2 x[G::KC * 8];
 #pragma unroll
         for (int k = 0; k < G::KC * 2; ++k) {
-          const uint32_t u[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+          const uint32_t u[4] = {raw[t][k].x, raw[t][k].y, raw[t][k].z, raw[t][k].w};
 #pragma unroll
           for (int z = 0; z < 4; ++z) {
             x[4 * k + z] = a.dtype == WNW_DTYPE_BF16 ? Pair<__nv_bfloat16>::get(u[z]) : Pair<__half>::get(u[z]);
@@ -510,6 +524,7 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
       }
 
       // ---- the warps' results meet ----
+      ask_rows(si + 1);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -588,7 +603,7 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
         }
         asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");   // read by all, free again
       }
-      if (!CLUSTER && tid == 0 && sg.slot == 1) a.part_head[blockIdx.x] = PartHead{sg.s, sg.h, sg.tile, sg.n_parts};
+      if (!CLUSTER && tid == 0 && sg.slot == 1) a.part_head[blockIdx.x] = PartHead{sg.r0, sg.n_seq, sg.h, sg.tile, sg.n_parts, {}};
       __syncthreads();
     }
   }
@@ -605,14 +620,32 @@ __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_consta
   pg_wait_for_stream();
   const PartHead ph = a.part_head[blockIdx.x];
   if (ph.n_parts < 2) return;
-  const int r0 = max(a.bv.starts[ph.s], 0), n = min(a.bv.starts[ph.s + 1], a.bv.n_rows) - r0, used = a.rt * a.g;
+  const int used = a.rt * a.g;
   const int part = threadIdx.x / LANES, d = threadIdx.x % LANES;
   for (int y = blockIdx.y; y < a.blocks * used; y += gridDim.y) {
     const int i = y / used, jj = y - i * used, j = i * a.rb + jj, tok = (ph.tile * a.blocks + i) * a.rt + jj / a.g, hd = jj % a.g;
-    if (tok >= n) continue;
+    if (tok >= ph.n) continue;
     auto at = [&](int k) { return ((long long)(blockIdx.x + k) * 2 + (k == 0)) * (a.blocks * a.rb) + j; };
+    constexpr int AHEAD = 8;                            // partial results on their way before the maxima are known
+    float4 xs[AHEAD];
+    PartRow rows[AHEAD];
+#pragma unroll
+    for (int z = 0; z < AHEAD; ++z) {
+      const int k = part + z * SPLIT;
+      rows[z] = PartRow{NOTHING, NOTHING, 0.f, 0.f};
+      xs[z] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (k < ph.n_parts) {
+        rows[z] = a.part_row[at(k)];
+        xs[z] = *reinterpret_cast<const float4 *>(a.part_o + at(k) * D + 4 * d);
+      }
+    }
     float mx = NOTHING, bx = NOTHING;
-    for (int k = threadIdx.x; k < ph.n_parts; k += 128) {
+#pragma unroll
+    for (int z = 0; z < AHEAD; ++z) {
+      mx = fmaxf(mx, rows[z].m);
+      bx = fmaxf(bx, rows[z].big_m);
+    }
+    for (int k = AHEAD * SPLIT + threadIdx.x; k < ph.n_parts; k += 128) {
       const PartRow pr = a.part_row[at(k)];
       mx = fmaxf(mx, pr.m);
       bx = fmaxf(bx, pr.big_m);
@@ -628,8 +661,14 @@ __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_consta
     bx = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
+#pragma unroll
+    for (int z = 0; z < AHEAD; ++z) {
+      const float by = ex2(rows[z].big_m - bx);
+      sum += rows[z].l * ex2(rows[z].m - mx);
+      acc.x += xs[z].x * by; acc.y += xs[z].y * by; acc.z += xs[z].z * by; acc.w += xs[z].w * by;
+    }
 #pragma unroll 4
-    for (int k = part; k < ph.n_parts; k += SPLIT) {
+    for (int k = part + AHEAD * SPLIT; k < ph.n_parts; k += SPLIT) {
       const PartRow pr = a.part_row[at(k)];
       const float4 x = *reinterpret_cast<const float4 *>(a.part_o + at(k) * D + 4 * d);
       const float by = ex2(pr.big_m - bx);
@@ -649,7 +688,7 @@ __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_consta
         acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
       }
       const float by = sum == 0.f ? 0.f : ex2(bx - mx) / sum;      // (no token: zeros)
-      const long long row = r0 + tok;
+      const long long row = ph.r0 + tok;
       const int head = ph.h * a.g + hd;
       unsigned char *p = a.out.p + 2 * (row * a.out.row + head * a.out.head + 4 * d);
       if (a.dtype == WNW_DTYPE_BF16) *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__nv_bfloat16>::put(acc.x * by, acc.y * by), Pair<__nv_bfloat16>::put(acc.z * by, acc.w * by));

@@ -8,7 +8,7 @@ constexpr float LAZY = 8.f;          // log2 by which a score may exceed the ref
 constexpr float NOTHING = -3e38f;    // the references before a token is seen: finite, so that differences are numbers
 
 // ---- workspace: per CTA two partial results (0: a head begun in an earlier CTA, 1: a head that ends in a later one) ----
-struct PartHead { int s, h, tile, n_parts; };  // of slot 1: whose, and how many CTAs share it; n_parts = 0: none
+struct PartHead { int r0, n, h, tile, n_parts, pad[3]; };  // of slot 1: rows of its sequence, which head and item, CTAs that share it (0: none)
 struct PartRow { float m, big_m, l, pad; };
 
 // A head's query rows come in items of `blocks` blocks: block i of item t holds query tokens [(t * blocks + i) * rt, ... + rt) in its

@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
   }
   pg_let_next_start();
   pg_wait_for_stream();
-  if (tid == 0) a.part_head[blockIdx.x] = PartHead{0, 0, 0, 0};
+  if (tid == 0) a.part_head[blockIdx.x] = PartHead{};
   const long long total = lay_out(a, sh);              // (its barriers order the above too)
   const long long len_line = (total + gridDim.x - 1) / gridDim.x, x0 = min(total, blockIdx.x * len_line), x1 = min(total, x0 + len_line);
   if (x0 >= x1) return;
@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
       if (tid == 0 && !whole && slot) {
         // the CTAs that this item runs over: it begins `before` tiles into this stretch
         const long long before = x1 - x0 - w.left;
-        a.part_head[blockIdx.x] = PartHead{w.s, w.h, w.t, (int)((before + w.need - 1) / len_line + 1)};
+        a.part_head[blockIdx.x] = PartHead{w.r0, w.n, w.h, w.t, (int)((before + w.need - 1) / len_line + 1), {}};
       }
     }
   } else if (wid < 12) {
