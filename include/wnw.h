@@ -464,7 +464,7 @@ wnw_status_t wnw_rotate(const wnw_rotate_t *call);
 enum { WNW_PAGES_E4M3 = 0, WNW_PAGES_INT8 = 1 };
 enum { WNW_PAGES_BAD_PAGE = 1,     /* a page id outside [0, n_pages): its rows were not written; read as zeros; not attended to */
        WNW_PAGES_BAD_LENGTH = 2,   /* a length or row range outside the table or the tensors: clipped to what is inside */
-       WNW_PAGES_TIMEOUT = 4 };    /* a copy did not arrive within the second that a kernel waits: the output is incomplete */
+       WNW_PAGES_TIMEOUT = 4 };    /* a copy did not arrive within the second that a kernel waits: rows that lack it are not-a-numbers */
 typedef struct {
   void *codes_dev;          /* DEVICE bytes [n_pages][n_kv_heads][2][page_tokens][head_dim]: K rows, then V rows; 16-byte aligned */
   float *scales_dev;        /* DEVICE [n_pages][n_kv_heads][2], powers of two */

@@ -122,7 +122,6 @@ __global__ void __launch_bounds__(THREADS, TURN ? 1 : (N == 4 ? 1536 : 1024) / T
   __shared__ uint32_t red[THREADS / 32];
   const PagesView &pv = a.pv;
   const int s = blockIdx.z, head = blockIdx.x >> 1, which = blockIdx.x & 1, tid = threadIdx.x;
-  pg_let_next_start();
   pg_wait_for_stream();
   const Span sp = span_of(pv, a.bv, s);
   if (sp.first >= sp.end) return;
@@ -256,7 +255,6 @@ __global__ void __launch_bounds__(256, 8) wnw_pages_read_kernel(const __grid_con
   constexpr int PPR = D / 8, N = 4;                    // pieces of eight codes of a row; of a thread in flight
   const PagesView &pv = a.pv;
   const int s = blockIdx.z, head = blockIdx.x >> 1, which = blockIdx.x & 1;
-  pg_let_next_start();
   pg_wait_for_stream();
   const Span sp = span_of(pv, a.bv, s);
   if (sp.first >= sp.end) return;
@@ -297,10 +295,12 @@ __global__ void __launch_bounds__(256, 8) wnw_pages_read_kernel(const __grid_con
   }
 }
 
-// Pages that a sequence's rows can touch, by what the caller says of the rows; the kernels' loops cover the rest.
+// CTAs along a sequence's pages: as many as its rows can touch, by what the caller says of the rows, but no more than eight times what the
+// sequences touch on average; the kernels' loops cover the rest.
 int pages_touched(const wnw_batch_t &b, int T) {
   const int rows = b.max_rows > 0 ? std::min(b.max_rows, b.n_rows) : b.n_rows;
-  return std::min((rows + T - 2) / T + 1, 65535);
+  const long long most = (rows + T - 2ll) / T + 1, mean = ((long long)b.n_rows / T + 2ll * b.n_seqs) / b.n_seqs + 1;
+  return (int)std::min({most, 8 * mean, 65535ll});
 }
 
 template <typename T, int D, int FMT, bool TURN> cudaError_t launch_write(const WriteArgs &a, dim3 grid, cudaStream_t st) {

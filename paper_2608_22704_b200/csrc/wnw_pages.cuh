@@ -90,7 +90,8 @@ wnw_status_t rotary_view(const wnw_rotary_t *r, int head_dim, int inverse, Rotar
 inline RowsView rows_view(const wnw_rows_t &r) { return RowsView{(unsigned char *)r.dev, (long long)r.row_stride, (long long)r.head_stride}; }
 
 // ---- launches that start while their predecessor on the stream ends ----
-// The next launch may be brought onto the SMs from here on; it waits itself before it touches anything.
+// The next launch may be brought onto the SMs from here on.  Only where that is this call's own, which waits before it touches anything: a
+// layer of a step whose queries are given in advance does not.
 __device__ __forceinline__ void pg_let_next_start() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
 // Everything before on the stream has completed.  By every CTA, before its first access to memory: then "completed" holds along chains.
 __device__ __forceinline__ void pg_wait_for_stream() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }

@@ -66,11 +66,12 @@ __device__ __forceinline__ void copy_granule(uint32_t dst, const CUtensorMap *ma
                ::"r"(dst), "l"(map), "r"(bar), "r"(0), "r"(row), "r"(block), "r"(page) : "memory");
 }
 // Bounded: gives up after about a second of SM clocks and says so, instead of hanging.
-__device__ __forceinline__ void wait_granule(uint32_t bar, uint32_t parity, const PagesView &pv) {
-  if (try_wait(bar, parity)) return;
+__device__ __forceinline__ bool wait_granule(uint32_t bar, uint32_t parity, const PagesView &pv) {
+  if (try_wait(bar, parity)) return true;
   const long long t0 = clock64();
   while (!try_wait(bar, parity))
-    if (clock64() - t0 > 2000000000ll) { pg_report(pv, WNW_PAGES_TIMEOUT); return; }
+    if (clock64() - t0 > 2000000000ll) { pg_report(pv, WNW_PAGES_TIMEOUT); return false; }
+  return true;
 }
 
 // W warps of a CTA, S granules of a warp in the ring.
@@ -167,7 +168,7 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
     asm volatile("prefetch.tensormap [%0];\n" ::"l"(&map) : "memory");
   }
   __syncwarp();
-  pg_let_next_start();
+  if (!CLUSTER) pg_let_next_start();
   pg_wait_for_stream();
   long long len_line = 0, x0 = 0, x1 = 0;
   int item0 = 0, n_items = 0;                           // CLUSTER: the tile of query tokens
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
         const uint32_t sc = ring_scale[w * S + stage];
         const unsigned char *src = ring + (w * S + stage) * G::STAGE;
         if (sc) {
-          wait_granule(bars_u + 8 * stage, phases >> stage & 1, pv);
+          if (!wait_granule(bars_u + 8 * stage, phases >> stage & 1, pv)) l[0][0] = l[0][1] = l[NT - 1][0] = l[NT - 1][1] = NAN;   // incomplete, and looks it
           phases ^= 1u << stage;
         }
         if (++stage == S) stage = 0;
@@ -616,7 +617,6 @@ __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_consta
   constexpr int LANES = D / 4, SPLIT = 128 / LANES;
   __shared__ float4 acc_s[SPLIT][LANES];
   __shared__ float sum_s[SPLIT], red[2][4];
-  pg_let_next_start();
   pg_wait_for_stream();
   const PartHead ph = a.part_head[blockIdx.x];
   if (ph.n_parts < 2) return;

@@ -466,6 +466,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
       }
 
       // ---- out ----
+      if (*(volatile int *)&sh.dead) l = NAN;          // incomplete, and looks it
       wait(&sh.o_done[i], n_mine - 1, sh, pv);
       fence_after();
       const bool whole = w.k0 == 0 && w.k1 == w.need;

@@ -63,7 +63,6 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(ROT_THREADS, 4) wnw_rotate_kernel(const __grid_constant__ RotateArgs a) {
   constexpr int N = VEC ? Vec<T>::N : 1, U = ROT_HEADS;
   extern __shared__ __align__(16) float2 cs[];          // [tokens_per_cta][N / 2][units][2], a unit's angles without bank conflicts; N = 1: [token][pair]
-  pg_let_next_start();
   pg_wait_for_stream();
   const int np = a.rot.n_pairs, units = np / N, t0 = blockIdx.x * a.tokens_per_cta, nt = min(a.tokens_per_cta, a.n_tokens - t0);
   const int pitch = np + 2;

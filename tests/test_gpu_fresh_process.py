@@ -91,3 +91,44 @@ def test_first_allocation_free_call_inside_a_capture():
         assert not wnw.wnw_attend_static_status()
         assert torch.equal(*outs) and outs[0].abs().max() > 0
     """)
+
+
+def test_calls_around_the_paged_store_first_inside_a_capture():
+    """Rotate, write, attend in its three forms and read back, each for the first time of the process inside a stream capture."""
+    _in_fresh_process("""
+        import torch
+        import paper_2608_22704_b200 as wnw
+        from pages_ref import Store, attention, attention_bounds
+        heads, hq, T, d, n = 2, 8, 16, 64, 200
+        gen = torch.Generator().manual_seed(5)
+        k, v = (torch.randn(n, heads, d, generator=gen).to(torch.bfloat16).cuda() for _ in range(2))
+        q = torch.randn(n, hq, d, generator=gen).to(torch.bfloat16).cuda()
+        ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        codes = torch.zeros(2000, heads, 2, T, d, dtype=torch.int8, device="cuda")
+        scales = torch.zeros(2000, heads, 2, device="cuda")
+        pages = wnw.wnw_pages(codes, scales)
+        table, wide, zero, full, one, all_ = ints([list(range(13))]), ints([list(range(2000))]), ints([0]), ints([n]), ints([0, 1]), ints([0, n])
+        plan, pos = wnw.wnw_rotary_init(32, 1e4), ints([list(range(n))])
+        turned, k2, v2 = (torch.empty_like(k) for _ in range(3))
+        outs = [torch.empty_like(q[:1]), torch.empty_like(q[:1]), torch.empty_like(q)]
+        ws = torch.empty(wnw.wnw_pages_attend_workspace(pages, hq), dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        with torch.cuda.graph(graph, stream=side):
+            wnw.wnw_rotate(plan, pos, k, turned)
+            wnw.wnw_pages_write(pages, table, zero, all_, k, v, rotary=plan, positions=pos)
+            wnw.wnw_pages_attend(pages, table, full, one, q[n - 1:], outs[0], ws)
+            wnw.wnw_pages_attend(pages, wide, full, one, q[n - 1:], outs[1], ws)
+            wnw.wnw_pages_attend(pages, table, full, all_, q, outs[2], ws)
+            wnw.wnw_pages_read(pages, table, zero, all_, k2, v2)
+        graph.replay()
+        torch.cuda.synchronize()
+        ref = Store(13, heads, T, d, 1)
+        ref.write([list(range(13))], [0], [n], [turned.double().cpu().numpy()], [v.double().cpu().numpy()])
+        want = ref.values(list(range(13)), n)
+        assert (k2.double().cpu().numpy() == want[0]).all() and (v2.double().cpu().numpy() == want[1]).all()
+        o, lse, spread, reach = attention(q.double().cpu().numpy(), want[0], want[1], list(range(1, n + 1)), d ** -0.5, T)
+        tol, _ = attention_bounds(o, lse, spread, reach, torch.bfloat16, d)
+        for got, rows in zip(outs, (slice(n - 1, n), slice(n - 1, n), slice(0, n))):
+            assert (abs(got.double().cpu().numpy() - o[rows]) <= tol[rows]).all()
+    """)

@@ -213,15 +213,16 @@ def test_write_row_by_row_is_write_of_all_where_the_scale_is_settled(fmt):
 
 
 @pytest.mark.parametrize("neighbours,pairs", [(False, 64), (True, 64), (False, 24), (True, 16)])
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
-def test_write_turns_keys_as_rotate_does(neighbours, pairs, dtype):
-    heads, d, T, rows = 3, 128, 64, [1, 100, 0, 64]
+@pytest.mark.parametrize("T,dtype", [(64, torch.bfloat16), (256, torch.float16), (16, torch.bfloat16), (128, torch.bfloat16)])
+def test_write_turns_keys_as_rotate_does(neighbours, pairs, T, dtype):
+    heads, d, rows = 3, 128, [1, 100, 0, 300]
     plan = wnw.wnw_rotary_init(pairs, 1e4, [pairs // 2, pairs - pairs // 2], neighbours=neighbours)
     pos = torch.randint(0, 10 ** 6, (2, sum(rows)), generator=torch.Generator().manual_seed(1), dtype=torch.int32).to(DEV)
     k, v = randn(sum(rows), heads, d, seed=3, dtype=dtype).to(DEV), randn(sum(rows), heads, d, seed=4, dtype=dtype).to(DEV)
     turned = torch.empty_like(k)
     wnw.wnw_rotate(plan, pos, k, turned)
-    b = Both(16, heads, T, d, INT8, 4, 4)
+    width = 310 // T + 1
+    b = Both(4 * width, heads, T, d, INT8, 4, width)
     b.write(k, v, rows, rotary=plan, positions=pos, k_ref=turned)
     b.check()
     b.write(k[:4], v[:4], [1] * 4, rotary=plan, positions=pos[:, :4], k_ref=turned[:4])
@@ -387,21 +388,26 @@ def test_attend_long_and_many(fmt, hq, heads, d):
     check_attention(out, lse, q, values_of(b, lengths), lengths, rows, True)
 
 
+@pytest.mark.parametrize("rows", [1, 30])
 @pytest.mark.parametrize("fmt", [E4M3, INT8])
-def test_attend_scales_far_apart(fmt):
-    """Pages whose values differ by 2^60, in both orders, and weights that the small ones carry."""
-    heads, T, d, n = 2, 16, 64, 160
-    for order in (1, -1):
-        b = Both(12, heads, T, d, fmt, 1, 10)
+def test_attend_scales_far_apart(fmt, rows):
+    """Pages whose values differ by 2^60, in both orders, and weights that the small ones carry; then pages of zeros among them."""
+    heads, T, d, n = 2, 16, 64, 640
+    for order in (1, -1, 0):
+        b = Both(42, heads, T, d, fmt, 1, 40)
         k, v = randn(n, heads, d, seed=1).to(DEV), randn(n, heads, d, seed=2).to(DEV)
         power = torch.arange(n // T, device=DEV).repeat_interleave(T).float()
-        power = (power if order > 0 else power.flip(0)) * 6 - 30
-        v = (v.float() * torch.exp2(power)[:, None, None]).to(torch.bfloat16)
+        power = (power if order > 0 else power.flip(0)) * 1.5 - 30
+        if order:
+            v = (v.float() * torch.exp2(power)[:, None, None]).to(torch.bfloat16)
+        else:
+            v[64:n - 64].view(-1, T, heads, d)[::2] = 0.0
+            v[n // 2:n - 16] = 0.0
         b.write(k, v, [n])
-        q = randn(1, 4, d, seed=3, scale=30.0).to(DEV)                # one key has nearly all the weight
+        q = randn(rows, 4, d, seed=3, scale=30.0).to(DEV)             # one key has nearly all the weight
         for scale in (0.0, 3.0, 1e-3):
-            out, lse = attend(b.pages, b.table_dev, [n], [1], q, scale=scale)
-            check_attention(out, lse, q, values_of(b, [n]), [n], [1], True, scale, T)
+            out, lse = attend(b.pages, b.table_dev, [n], [rows], q, scale=scale)
+            check_attention(out, lse, q, values_of(b, [n]), [n], [rows], True, scale, T)
 
 
 @pytest.mark.parametrize("dtype,size,scale", [(torch.bfloat16, 1e25, 1e-26), (torch.bfloat16, 1e-25, 1e24), (torch.float16, 6e4, 1e-5), (torch.bfloat16, 0.0, 0.0)])
@@ -494,14 +500,28 @@ def test_strides_of_queries_and_outputs():
     assert torch.equal(again, want)
 
 
-def test_attend_gives_the_same_bits_again():
-    lengths = [5000, 123, 777]
+@pytest.mark.parametrize("lengths,rows", [([5000, 123, 777], 1), ([40000], 1), ([5000, 123, 777], 70)])
+def test_attend_gives_the_same_bits_again(lengths, rows):
     b = filled(E4M3, 4, 64, 128, lengths)
-    q = randn(3, 16, 128, seed=3, scale=2.0).to(DEV)
-    first = attend(b.pages, b.table_dev, lengths, [1] * 3, q)
+    q = randn(rows * len(lengths), 16, 128, seed=3, scale=2.0).to(DEV)
+    first = attend(b.pages, b.table_dev, lengths, [rows] * len(lengths), q)
     for _ in range(5):
-        again = attend(b.pages, b.table_dev, lengths, [1] * 3, q)
+        again = attend(b.pages, b.table_dev, lengths, [rows] * len(lengths), q)
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_attend_in_clusters_and_on_the_line():
+    """Short sequences under a table of any width: what the call may have to read decides how it is cut, not what it gives."""
+    lengths = [300, 17, 0, 1]
+    b = filled(INT8, 2, 64, 128, lengths)
+    for rows, hq in ((1, 8), (3, 10)):
+        q = randn(4 * rows, hq, 128, seed=3, scale=2.0).to(DEV)
+        for width in (b.table_dev.shape[1], 40, 4000):
+            table = torch.full((4, width), 10 ** 9, dtype=torch.int32, device=DEV)         # never looked at
+            table[:, :b.table_dev.shape[1]] = b.table_dev
+            out, lse = attend(b.pages, table, lengths, [rows] * 4, q, max_rows=rows)
+            check_attention(out, lse, q, values_of(b, lengths), lengths, [rows] * 4, True)
+    assert b.status.item() == 0
 
 
 def test_a_captured_step_replayed_while_sequences_grow():
