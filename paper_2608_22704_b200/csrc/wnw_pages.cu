@@ -79,33 +79,31 @@ struct WriteArgs {
   RotaryView rot;                    // n_pairs = 0: keys are written as they are
   const int32_t *positions;
   long long axis_stride;
+  int heads;                         // of K that share a CTA where keys are turned
+  bool values_only;
 };
 
+constexpr int TURN_HEADS = 4;
 // Keys that are turned: a thread takes 8 elements from `lo` on and 8 from `hi` on, so that the turn of a pair stays with it.
 template <int D> __device__ __forceinline__ void unit_offsets(int u, int n_pairs, int neighbours, int *lo, int *hi) {
   const int turned = n_pairs / 8;
   if (u < turned && !neighbours) { *lo = 8 * u; *hi = 8 * u + n_pairs; }
   else { *lo = 16 * u; *hi = 16 * u + 8; }             // also what lies behind the pairs: 2 * n_pairs + 16 * (u - turned)
 }
-// 16 elements of a row turned by its position; p0: the first of their eight pairs
-struct Plan { double turns[128]; int axis[128]; };     // in shared memory: lanes want different pairs
-template <typename T> __device__ __forceinline__ void turn_unit(const WriteArgs &a, const Plan &plan, int row, int p0, uint4 &lo, uint4 &hi) {
-  auto angle = [&](int p) { return pg_angle(plan.turns[p], a.positions[plan.axis[p] * a.axis_stride + row]); };
+// 16 elements of a row turned by the angles of their eight pairs
+template <typename T> __device__ __forceinline__ void turn_unit(bool neighbours, const float2 (&c)[8], uint4 &lo, uint4 &hi) {
   uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-  if (a.rot.neighbours) {
+  if (neighbours) {
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-      const float2 c = angle(p0 + q);
-      const float2 f = Pair<T>::get(w[q]), t = pg_turn(f.x, f.y, c);
+      const float2 f = Pair<T>::get(w[q]), t = pg_turn(f.x, f.y, c[q]);
       w[q] = Pair<T>::put(t.x, t.y);
     }
   } else {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const float2 c = angle(p0 + 2 * q);
-      const float2 d = angle(p0 + 2 * q + 1);
       const float2 f = Pair<T>::get(w[q]), g = Pair<T>::get(w[4 + q]);
-      const float2 t = pg_turn(f.x, g.x, c), z = pg_turn(f.y, g.y, d);
+      const float2 t = pg_turn(f.x, g.x, c[2 * q]), z = pg_turn(f.y, g.y, c[2 * q + 1]);
       w[q] = Pair<T>::put(t.x, z.x);
       w[4 + q] = Pair<T>::put(t.y, z.y);
     }
@@ -114,20 +112,25 @@ template <typename T> __device__ __forceinline__ void turn_unit(const WriteArgs 
   hi = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
-// CTA: (pages of a sequence, one at a time; KV head and K|V; sequence).  A thread keeps its N pieces of eight elements in registers from the
+// CTA: (KV head and K|V; pages of a sequence, one at a time; sequence).  Where keys are turned, `heads` heads of K share a CTA: its threads
+// keep the angles of their pieces' pairs from one to the next.  A thread keeps its N pieces of eight elements in registers from the
 // one pass over the rows to the codes; 1536 threads an SM instead of 1024 make 78 MB of them 59 -> 53 us.
 template <typename T, int D, int FMT, int N, int THREADS, bool TURN>
-__global__ void __launch_bounds__(THREADS, TURN ? 1 : (N == 4 ? 1536 : 1024) / THREADS) wnw_pages_write_kernel(const __grid_constant__ WriteArgs a) {
+__global__ void __launch_bounds__(THREADS, (TURN || N == 8 ? 1024 : 1536) / THREADS) wnw_pages_write_kernel(const __grid_constant__ WriteArgs a) {
   constexpr int PPR = D / 8;                           // pieces of a row
   __shared__ uint32_t red[THREADS / 32];
   const PagesView &pv = a.pv;
-  const int s = blockIdx.z, head = blockIdx.x >> 1, which = blockIdx.x & 1, tid = threadIdx.x;
+  const int s = blockIdx.z, tid = threadIdx.x, n_turned = TURN ? (pv.H + a.heads - 1) / a.heads : 0;
+  const int which = TURN ? blockIdx.x >= n_turned : a.values_only ? 1 : blockIdx.x & 1;
+  const int head_0 = TURN ? (which ? blockIdx.x - n_turned : blockIdx.x * a.heads) : a.values_only ? blockIdx.x : blockIdx.x >> 1;
+  const int head_1 = TURN && !which ? min(pv.H, head_0 + a.heads) : head_0 + 1;
   pg_wait_for_stream();
   const Span sp = span_of(pv, a.bv, s);
   if (sp.first >= sp.end) return;
-  __shared__ Plan plan;
+  __shared__ double turns[TURN ? 128 : 1];             // the plan: lanes want different pairs, the kernel's parameters are read one at a time
+  __shared__ int axis[TURN ? 128 : 1];
   if (TURN && which == 0) {
-    for (int p = tid; p < a.rot.n_pairs; p += THREADS) { plan.turns[p] = a.rot.turns[p]; plan.axis[p] = a.rot.axis[p]; }
+    for (int p = tid; p < a.rot.n_pairs; p += THREADS) { turns[p] = a.rot.turns[p]; axis[p] = a.rot.axis[p]; }
     __syncthreads();
   }
   const int page0 = sp.first / pv.T, n_touched = (sp.end - 1) / pv.T - page0 + 1;
@@ -149,95 +152,103 @@ __global__ void __launch_bounds__(THREADS, TURN ? 1 : (N == 4 ? 1536 : 1024) / T
     const int base = (page0 + i) * pv.T, t0 = max(sp.first, base) - base, t1 = min(sp.end - base, pv.T), rows = t1 - t0;
     const int page = a.bv.table[(long long)s * a.bv.stride + page0 + i];
     const int row0 = sp.row0 + base + t0 - sp.first;
-    const T *in = reinterpret_cast<const T *>(a.in[which].p) + (long long)row0 * a.in[which].row + head * a.in[which].head;
-    uint4 x[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      int r, e;
-      piece(j, &r, &e);
-      x[j] = r < rows ? *reinterpret_cast<const uint4 *>(in + r * a.in[which].row + e) : make_uint4(0, 0, 0, 0);
-    }
-    if (page < 0 || page >= pv.n_pages) {
-      if (tid == 0) pg_report(pv, WNW_PAGES_BAD_PAGE);
-      continue;
-    }
-    float *scale = pv.scales + page * pv.scale_stride + head * 2 + which;
-    const float old_scale = t0 ? *scale : 0.f;         // needed late, asked for early
+    float2 angles[TURN ? N / 2 : 1][8];
     if (TURN && which == 0) {
 #pragma unroll
-      for (int j = 0; j < N; j += 2) {
-        const int u = tid + (j >> 1) * THREADS, p0 = 8 * (u % (PPR / 2)), r = u / (PPR / 2);
-        if (r < rows && p0 < a.rot.n_pairs) turn_unit<T>(a, plan, row0 + r, p0, x[j], x[j + 1]);
+      for (int j = 0; j < N / 2; ++j) {
+        const int u = tid + j * THREADS, p0 = 8 * (u % (PPR / 2)), r = u / (PPR / 2);
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          angles[j][q] = r < rows && p0 < a.rot.n_pairs ? pg_angle(turns[p0 + q], a.positions[axis[p0 + q] * a.axis_stride + row0 + r]) : make_float2(1.f, 0.f);
       }
     }
-    // The largest magnitude: as integers, two at a time, while all are finite
-    uint32_t both = 0;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      both = __vmaxu2(both, __vmaxu2(__vmaxu2(x[j].x & 0x7fff7fffu, x[j].y & 0x7fff7fffu), __vmaxu2(x[j].z & 0x7fff7fffu, x[j].w & 0x7fff7fffu)));
-    }
-    const uint32_t top = max(both & 0xffffu, both >> 16);
-    const bool odd = top >= Bits<T>::INF;               // the thread's elements are not all finite
-    uint32_t most = Bits<T>::as_float(top);
-    if (odd) {
-      most = 0;
+    if ((page < 0 || page >= pv.n_pages) && tid == 0) pg_report(pv, WNW_PAGES_BAD_PAGE);
+    if (page < 0 || page >= pv.n_pages) continue;
+    for (int head = head_0; head < head_1; ++head) {
+      const T *in = reinterpret_cast<const T *>(a.in[which].p) + (long long)row0 * a.in[which].row + head * a.in[which].head;
+      uint4 x[N];
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const uint32_t m = w[q >> 1] >> 16 * (q & 1) & 0x7fffu;
-          most = max(most, m < Bits<T>::INF ? Bits<T>::as_float(m) : 0u);
-        }
+        int r, e;
+        piece(j, &r, &e);
+        x[j] = r < rows ? *reinterpret_cast<const uint4 *>(in + r * a.in[which].row + e) : make_uint4(0, 0, 0, 0);
       }
-    }
-    most = __reduce_max_sync(0xffffffffu, most);
-    if ((tid & 31) == 0) red[tid >> 5] = most;
-    __syncthreads();
+      float *scale = pv.scales + page * pv.scale_stride + head * 2 + which;
+      const float old_scale = t0 ? *scale : 0.f;         // needed late, asked for early
+      if (TURN && which == 0) {
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) most = max(most, red[w]);
-    __syncthreads();                                   // red is free for the next page
-    int e_new = exponent_for<FMT>(most);
-    unsigned char *block = pv.codes + page * pv.page_stride + (long long)(head * 2 + which) * pv.T * D;
-    if (t0) {
-      const int had = max(PG_LOWEST, min(pg_highest(FMT), (int)(__float_as_uint(old_scale) >> 23 & 255) - 127));
-      if (e_new > had) {                               // rows of before, for the raised scale
-        const float down = power(max(-64, had - e_new));   // (codes / 2^64 are 0 already)
-        for (int u = tid; u < t0 * (D / 16); u += THREADS) {
-          uint4 *p = reinterpret_cast<uint4 *>(block + (long long)u * 16), v = *p;
-          uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            float f[4];
-            decode4<FMT>(w[q], f);
-            w[q] = encode4<FMT>(f[0] * down, f[1] * down, f[2] * down, f[3] * down);
-          }
-          *p = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        for (int j = 0; j < N; j += 2)
+          if (8 * ((tid + (j >> 1) * THREADS) % (PPR / 2)) < a.rot.n_pairs) turn_unit<T>(a.rot.neighbours, angles[j >> 1], x[j], x[j + 1]);
       }
-      e_new = max(e_new, had);
-    }
-    if (tid == 0) *scale = power(e_new);
-    const float by = power(-e_new);
-    const bool plain = !odd && e_new < pg_highest(FMT);   // no code beyond the largest
+      // The largest magnitude: as integers, two at a time, while all are finite
+      uint32_t both = 0;
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      int r, e;
-      piece(j, &r, &e);
-      if (r < rows) {
-        const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-        uint32_t c[2];
+      for (int j = 0; j < N; ++j) {
+        both = __vmaxu2(both, __vmaxu2(__vmaxu2(x[j].x & 0x7fff7fffu, x[j].y & 0x7fff7fffu), __vmaxu2(x[j].z & 0x7fff7fffu, x[j].w & 0x7fff7fffu)));
+      }
+      const uint32_t top = max(both & 0xffffu, both >> 16);
+      const bool odd = top >= Bits<T>::INF;               // the thread's elements are not all finite
+      uint32_t most = Bits<T>::as_float(top);
+      if (odd) {
+        most = 0;
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const float2 f = Pair<T>::get(w[2 * q]), g = Pair<T>::get(w[2 * q + 1]);
-          if (FMT == WNW_PAGES_INT8 && plain) {          // rounded where it is added to 1.5 * 2^23: the integer is the sum's low byte
-            const float u = __fmaf_rn(f.x, by, 12582912.f), v = __fmaf_rn(f.y, by, 12582912.f), y = __fmaf_rn(g.x, by, 12582912.f), z = __fmaf_rn(g.y, by, 12582912.f);
-            c[q] = __byte_perm(__byte_perm(__float_as_uint(u), __float_as_uint(v), 0x0040), __byte_perm(__float_as_uint(y), __float_as_uint(z), 0x0040), 0x5410);
-          } else {
-            c[q] = encode4<FMT>(f.x * by, f.y * by, g.x * by, g.y * by);
+        for (int j = 0; j < N; ++j) {
+          const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const uint32_t m = w[q >> 1] >> 16 * (q & 1) & 0x7fffu;
+            most = max(most, m < Bits<T>::INF ? Bits<T>::as_float(m) : 0u);
           }
         }
-        *reinterpret_cast<uint2 *>(block + (t0 + r) * D + e) = make_uint2(c[0], c[1]);
+      }
+      most = __reduce_max_sync(0xffffffffu, most);
+      if ((tid & 31) == 0) red[tid >> 5] = most;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < THREADS / 32; ++w) most = max(most, red[w]);
+      __syncthreads();                                   // red is free for the next page
+      int e_new = exponent_for<FMT>(most);
+      unsigned char *block = pv.codes + page * pv.page_stride + (long long)(head * 2 + which) * pv.T * D;
+      if (t0) {
+        const int had = max(PG_LOWEST, min(pg_highest(FMT), (int)(__float_as_uint(old_scale) >> 23 & 255) - 127));
+        if (e_new > had) {                               // rows of before, for the raised scale
+          const float down = power(max(-64, had - e_new));   // (codes / 2^64 are 0 already)
+          for (int u = tid; u < t0 * (D / 16); u += THREADS) {
+            uint4 *p = reinterpret_cast<uint4 *>(block + (long long)u * 16), v = *p;
+            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float f[4];
+              decode4<FMT>(w[q], f);
+              w[q] = encode4<FMT>(f[0] * down, f[1] * down, f[2] * down, f[3] * down);
+            }
+            *p = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+        e_new = max(e_new, had);
+      }
+      if (tid == 0) *scale = power(e_new);
+      const float by = power(-e_new);
+      const bool plain = !odd && e_new < pg_highest(FMT);   // no code beyond the largest
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        int r, e;
+        piece(j, &r, &e);
+        if (r < rows) {
+          const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+          uint32_t c[2];
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const float2 f = Pair<T>::get(w[2 * q]), g = Pair<T>::get(w[2 * q + 1]);
+            if (FMT == WNW_PAGES_INT8 && plain) {          // rounded where it is added to 1.5 * 2^23: the integer is the sum's low byte
+              const float u = __fmaf_rn(f.x, by, 12582912.f), v = __fmaf_rn(f.y, by, 12582912.f), y = __fmaf_rn(g.x, by, 12582912.f), z = __fmaf_rn(g.y, by, 12582912.f);
+              c[q] = __byte_perm(__byte_perm(__float_as_uint(u), __float_as_uint(v), 0x0040), __byte_perm(__float_as_uint(y), __float_as_uint(z), 0x0040), 0x5410);
+            } else {
+              c[q] = encode4<FMT>(f.x * by, f.y * by, g.x * by, g.y * by);
+            }
+          }
+          *reinterpret_cast<uint2 *>(block + (t0 + r) * D + e) = make_uint2(c[0], c[1]);
+        }
       }
     }
   }
@@ -310,12 +321,24 @@ template <typename T, int D, int FMT, bool TURN> cudaError_t launch_write(const 
   if (pieces <= 2048) return pg_launch(wnw_pages_write_kernel<T, D, FMT, 8, 256, TURN>, grid, 256, 0, st, 0, a);
   return pg_launch(wnw_pages_write_kernel<T, D, FMT, 8, 512, TURN>, grid, 512, 0, st, 0, a);
 }
-template <typename T, int D, int FMT> cudaError_t launch_write(const WriteArgs &a, dim3 grid, cudaStream_t st) {
-  return a.rot.n_pairs ? launch_write<T, D, FMT, true>(a, grid, st) : launch_write<T, D, FMT, false>(a, grid, st);
+// Angles are the larger part of turning a key, and the same for all heads, so that several share a CTA, and the values go by themselves (the
+// kernel that turns has registers for fewer threads): 30000 tokens of 8 heads of 128, a head a CTA 91 us, four 78, the values apart 66, 1024
+// threads an SM 57; wnw_rotate and then a write take 60.  A few new rows are done soonest a head a CTA, values in the same launch.
+template <typename T, int D, int FMT> cudaError_t launch_write(WriteArgs &a, int max_rows, dim3 grid, cudaStream_t st) {
+  a.values_only = false;
+  if (!a.rot.n_pairs) { grid.x = 2 * a.pv.H; return launch_write<T, D, FMT, false>(a, grid, st); }
+  const bool few = max_rows > 0 && max_rows <= 8;
+  a.heads = few ? 1 : TURN_HEADS;
+  grid.x = (a.pv.H + a.heads - 1) / a.heads + (few ? a.pv.H : 0);
+  const cudaError_t e = launch_write<T, D, FMT, true>(a, grid, st);
+  if (few || e != cudaSuccess) return e;
+  a.values_only = true;
+  grid.x = a.pv.H;
+  return launch_write<T, D, FMT, false>(a, grid, st);
 }
-template <typename T> cudaError_t launch_write(const WriteArgs &a, int d, int fmt, dim3 grid, cudaStream_t st) {
-  if (d == 64) return fmt == WNW_PAGES_E4M3 ? launch_write<T, 64, WNW_PAGES_E4M3>(a, grid, st) : launch_write<T, 64, WNW_PAGES_INT8>(a, grid, st);
-  return fmt == WNW_PAGES_E4M3 ? launch_write<T, 128, WNW_PAGES_E4M3>(a, grid, st) : launch_write<T, 128, WNW_PAGES_INT8>(a, grid, st);
+template <typename T> cudaError_t launch_write(WriteArgs &a, int d, int fmt, int max_rows, dim3 grid, cudaStream_t st) {
+  if (d == 64) return fmt == WNW_PAGES_E4M3 ? launch_write<T, 64, WNW_PAGES_E4M3>(a, max_rows, grid, st) : launch_write<T, 64, WNW_PAGES_INT8>(a, max_rows, grid, st);
+  return fmt == WNW_PAGES_E4M3 ? launch_write<T, 128, WNW_PAGES_E4M3>(a, max_rows, grid, st) : launch_write<T, 128, WNW_PAGES_INT8>(a, max_rows, grid, st);
 }
 template <typename T> cudaError_t launch_read(const ReadArgs &a, int d, int fmt, dim3 grid, cudaStream_t st) {
   if (d == 64) return pg_launch(fmt == WNW_PAGES_E4M3 ? wnw_pages_read_kernel<T, 64, WNW_PAGES_E4M3> : wnw_pages_read_kernel<T, 64, WNW_PAGES_INT8>, grid, 256, 0, st, 0, a);
@@ -394,10 +417,10 @@ extern "C" wnw_status_t wnw_pages_write(const wnw_pages_rows_t *call) {
   if (!call->batch.n_seqs || !call->batch.n_rows) return WNW_OK;
   OnDevice on(call->pages->device);
   if (!on.ok) return WNW_ERR_CUDA;
-  const dim3 grid(2 * a.pv.H, pages_touched(call->batch, a.pv.T), call->batch.n_seqs);   // (a token's heads lie beside one another)
+  const dim3 grid(1, pages_touched(call->batch, a.pv.T), call->batch.n_seqs);            // x: heads (a token's lie beside one another)
   const cudaStream_t st = (cudaStream_t)call->cuda_stream;
-  const int d = call->pages->head_dim, fmt = call->pages->format;
-  const cudaError_t e = call->dtype == WNW_DTYPE_BF16 ? launch_write<__nv_bfloat16>(a, d, fmt, grid, st) : launch_write<__half>(a, d, fmt, grid, st);
+  const int d = call->pages->head_dim, fmt = call->pages->format, rows = call->batch.max_rows;
+  const cudaError_t e = call->dtype == WNW_DTYPE_BF16 ? launch_write<__nv_bfloat16>(a, d, fmt, rows, grid, st) : launch_write<__half>(a, d, fmt, rows, grid, st);
   return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
 }
 
