@@ -37,6 +37,19 @@ template <int FMT> __device__ __forceinline__ void decode4(uint32_t w, float (&x
     x[2] = (float)(int)(signed char)(w >> 16); x[3] = (float)((int)w >> 24);
   }
 }
+// Four codes times their scale.  int8: code + 128 as the low byte of an fp32 number from 2^23 on, times the scale, less (2^23 + 128) times the
+// scale (`from`): one rounding, of a number that fp32 holds.  (As far as it holds `from` too.)
+template <int FMT> __device__ __forceinline__ void scaled4(uint32_t w, float scale, float from, float (&x)[4]) {
+  if (FMT == WNW_PAGES_E4M3 || from == -INFINITY) {
+    decode4<FMT>(w, x);
+#pragma unroll
+    for (int z = 0; z < 4; ++z) x[z] *= scale;
+  } else {
+    w ^= 0x80808080u;
+#pragma unroll
+    for (int z = 0; z < 4; ++z) x[z] = __fmaf_rn(__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7440 + z)), scale, from);
+  }
+}
 // the scale's exponent for rows whose largest magnitude has these bits
 template <int FMT> __device__ __forceinline__ int exponent_for(uint32_t bits) {
   // 448 = 1.75 * 2^8; 127 = 1.984375 * 2^6
@@ -116,7 +129,7 @@ template <typename T> __device__ __forceinline__ void turn_unit(bool neighbours,
 // keep the angles of their pieces' pairs from one to the next.  A thread keeps its N pieces of eight elements in registers from the
 // one pass over the rows to the codes; 1536 threads an SM instead of 1024 make 78 MB of them 59 -> 53 us.
 template <typename T, int D, int FMT, int N, int THREADS, bool TURN>
-__global__ void __launch_bounds__(THREADS, (TURN || N == 8 ? 1024 : 1536) / THREADS) wnw_pages_write_kernel(const __grid_constant__ WriteArgs a) {
+__global__ void __launch_bounds__(THREADS, (TURN && N == 8 ? 512 : TURN || N == 8 ? 1024 : 1536) / THREADS) wnw_pages_write_kernel(const __grid_constant__ WriteArgs a) {
   constexpr int PPR = D / 8;                           // pieces of a row
   __shared__ uint32_t red[THREADS / 32];
   const PagesView &pv = a.pv;
@@ -276,6 +289,8 @@ __global__ void __launch_bounds__(256, 8) wnw_pages_read_kernel(const __grid_con
     const bool there = page >= 0 && page < pv.n_pages;
     if (!there && threadIdx.x == 0) pg_report(pv, WNW_PAGES_BAD_PAGE);
     const float scale = there ? pv.scales[page * pv.scale_stride + head * 2 + which] : 0.f;
+    const bool large = std::is_same<T, __half>::value && scale > 128.f;      // beyond fp16: 448 * 2^8 on, 127 * 2^10 on
+    const float from = -8388736.f * scale;
     const unsigned char *block = pv.codes + (there ? page : 0) * pv.page_stride + ((long long)(head * 2 + which) * pv.T + t0) * D;
     T *out = reinterpret_cast<T *>(a.out[which].p) + (long long)(sp.row0 + base + t0 - sp.first) * a.out[which].row + head * a.out[which].head;
     const int all = (t1 - t0) * PPR;
@@ -291,12 +306,12 @@ __global__ void __launch_bounds__(256, 8) wnw_pages_read_kernel(const __grid_con
         const int u = u0 + 256 * k;
         if (u < all) {
           float f[8];
-          decode4<FMT>(v[k].x, reinterpret_cast<float (&)[4]>(f[0]));
-          decode4<FMT>(v[k].y, reinterpret_cast<float (&)[4]>(f[4]));
+          scaled4<FMT>(v[k].x, scale, from, reinterpret_cast<float (&)[4]>(f[0]));
+          scaled4<FMT>(v[k].y, scale, from, reinterpret_cast<float (&)[4]>(f[4]));
+          if (large) {
 #pragma unroll
-          for (int z = 0; z < 8; ++z) {
-            f[z] *= scale;
-            if (std::is_same<T, __half>::value && fabsf(f[z]) > 65504.f) f[z] = copysignf(65504.f, f[z]);
+            for (int z = 0; z < 8; ++z)
+              if (fabsf(f[z]) > 65504.f) f[z] = copysignf(65504.f, f[z]);
           }
           *reinterpret_cast<uint4 *>(out + (long long)(u / PPR) * a.out[which].row + u % PPR * 8) =
               make_uint4(Pair<T>::put(f[0], f[1]), Pair<T>::put(f[2], f[3]), Pair<T>::put(f[4], f[5]), Pair<T>::put(f[6], f[7]));

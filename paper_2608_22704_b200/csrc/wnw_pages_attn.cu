@@ -610,22 +610,65 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
   }
 }
 
-// A head that several CTAs share: CTA (b, y) puts every gridDim.y-th row of the head together that begins in CTA b of the attention and
-// does not end there.
+// A head that several CTAs share: CTA (b, y) puts rows of the head together that begins in CTA b of the attention and does not end there.
+// Up to FEW partial results are read by every thread for itself, a row by D / 4 of them; more are dealt out over the CTA's threads, which
+// then take a row together.
 template <int D>
 __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_constant__ AttendArgs a) {
-  constexpr int LANES = D / 4, SPLIT = 128 / LANES;
+  constexpr int LANES = D / 4, SPLIT = 128 / LANES, FEW = 8;
   __shared__ float4 acc_s[SPLIT][LANES];
   __shared__ float sum_s[SPLIT], red[2][4];
   pg_wait_for_stream();
   const PartHead ph = a.part_head[blockIdx.x];
   if (ph.n_parts < 2) return;
-  const int used = a.rt * a.g;
-  const int part = threadIdx.x / LANES, d = threadIdx.x % LANES;
-  for (int y = blockIdx.y; y < a.blocks * used; y += gridDim.y) {
-    const int i = y / used, jj = y - i * used, j = i * a.rb + jj, tok = (ph.tile * a.blocks + i) * a.rt + jj / a.g, hd = jj % a.g;
-    if (tok >= ph.n) continue;
-    auto at = [&](int k) { return ((long long)(blockIdx.x + k) * 2 + (k == 0)) * (a.blocks * a.rb) + j; };
+  const int used = a.rt * a.g, all = a.blocks * used, part = threadIdx.x / LANES, d = threadIdx.x % LANES;
+  // Row y of the head: its place in the partial results, its row of the batch and query head; false: no such token
+  auto place = [&](int y, int *j, long long *row, int *head) {
+    const int i = y / used, jj = y - i * used, tok = (ph.tile * a.blocks + i) * a.rt + jj / a.g;
+    *j = i * a.rb + jj;
+    *row = ph.r0 + tok;
+    *head = ph.h * a.g + jj % a.g;
+    return tok < ph.n;
+  };
+  auto at = [&](int k, int j) { return ((long long)(blockIdx.x + k) * 2 + (k == 0)) * (a.blocks * a.rb) + j; };
+  auto put = [&](float4 acc, float sum, float mx, float bx, long long row, int head) {
+    const float by = sum == 0.f ? 0.f : ex2(bx - mx) / sum;        // (no token: zeros)
+    unsigned char *p = a.out.p + 2 * (row * a.out.row + head * a.out.head + 4 * d);
+    if (a.dtype == WNW_DTYPE_BF16) *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__nv_bfloat16>::put(acc.x * by, acc.y * by), Pair<__nv_bfloat16>::put(acc.z * by, acc.w * by));
+    else *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__half>::put(acc.x * by, acc.y * by), Pair<__half>::put(acc.z * by, acc.w * by));
+    if (a.lse && d == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718055994531f;
+  };
+  int j, head;
+  long long row;
+  if (ph.n_parts <= FEW) {
+    for (int y = blockIdx.y * SPLIT + part; y < all; y += gridDim.y * SPLIT) {
+      if (!place(y, &j, &row, &head)) continue;
+      float4 xs[FEW];
+      PartRow rows[FEW];
+#pragma unroll
+      for (int k = 0; k < FEW; ++k)
+        if (k < ph.n_parts) {
+          rows[k] = a.part_row[at(k, j)];
+          xs[k] = *reinterpret_cast<const float4 *>(a.part_o + at(k, j) * D + 4 * d);
+        }
+      float mx = NOTHING, bx = NOTHING, sum = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < FEW; ++k)
+        if (k < ph.n_parts) { mx = fmaxf(mx, rows[k].m); bx = fmaxf(bx, rows[k].big_m); }
+#pragma unroll
+      for (int k = 0; k < FEW; ++k)
+        if (k < ph.n_parts) {
+          const float by = ex2(rows[k].big_m - bx);
+          sum += rows[k].l * ex2(rows[k].m - mx);
+          acc.x += xs[k].x * by; acc.y += xs[k].y * by; acc.z += xs[k].z * by; acc.w += xs[k].w * by;
+        }
+      put(acc, sum, mx, bx, row, head);
+    }
+    return;
+  }
+  for (int y = blockIdx.y; y < all; y += gridDim.y) {
+    if (!place(y, &j, &row, &head)) continue;
     constexpr int AHEAD = 8;                            // partial results on their way before the maxima are known
     float4 xs[AHEAD];
     PartRow rows[AHEAD];
@@ -635,8 +678,8 @@ __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_consta
       rows[z] = PartRow{NOTHING, NOTHING, 0.f, 0.f};
       xs[z] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (k < ph.n_parts) {
-        rows[z] = a.part_row[at(k)];
-        xs[z] = *reinterpret_cast<const float4 *>(a.part_o + at(k) * D + 4 * d);
+        rows[z] = a.part_row[at(k, j)];
+        xs[z] = *reinterpret_cast<const float4 *>(a.part_o + at(k, j) * D + 4 * d);
       }
     }
     float mx = NOTHING, bx = NOTHING;
@@ -646,7 +689,7 @@ __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_consta
       bx = fmaxf(bx, rows[z].big_m);
     }
     for (int k = AHEAD * SPLIT + threadIdx.x; k < ph.n_parts; k += 128) {
-      const PartRow pr = a.part_row[at(k)];
+      const PartRow pr = a.part_row[at(k, j)];
       mx = fmaxf(mx, pr.m);
       bx = fmaxf(bx, pr.big_m);
     }
@@ -669,8 +712,8 @@ __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_consta
     }
 #pragma unroll 4
     for (int k = part + AHEAD * SPLIT; k < ph.n_parts; k += SPLIT) {
-      const PartRow pr = a.part_row[at(k)];
-      const float4 x = *reinterpret_cast<const float4 *>(a.part_o + at(k) * D + 4 * d);
+      const PartRow pr = a.part_row[at(k, j)];
+      const float4 x = *reinterpret_cast<const float4 *>(a.part_o + at(k, j) * D + 4 * d);
       const float by = ex2(pr.big_m - bx);
       sum += pr.l * ex2(pr.m - mx);
       acc.x += x.x * by; acc.y += x.y * by; acc.z += x.z * by; acc.w += x.w * by;
@@ -687,13 +730,7 @@ __global__ void __launch_bounds__(128) wnw_pages_join_kernel(const __grid_consta
         sum += sum_s[k];
         acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
       }
-      const float by = sum == 0.f ? 0.f : ex2(bx - mx) / sum;      // (no token: zeros)
-      const long long row = ph.r0 + tok;
-      const int head = ph.h * a.g + hd;
-      unsigned char *p = a.out.p + 2 * (row * a.out.row + head * a.out.head + 4 * d);
-      if (a.dtype == WNW_DTYPE_BF16) *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__nv_bfloat16>::put(acc.x * by, acc.y * by), Pair<__nv_bfloat16>::put(acc.z * by, acc.w * by));
-      else *reinterpret_cast<uint2 *>(p) = make_uint2(Pair<__half>::put(acc.x * by, acc.y * by), Pair<__half>::put(acc.z * by, acc.w * by));
-      if (a.lse && d == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718055994531f;
+      put(acc, sum, mx, bx, row, head);
     }
     __syncthreads();
   }
@@ -841,7 +878,7 @@ extern "C" wnw_status_t wnw_pages_attend(const wnw_pages_attend_t *call) {
     else e = pages->format == WNW_PAGES_E4M3 ? launch<128, WNW_PAGES_E4M3>(a, map, nt, n_ctas, cluster, pages->device, st) : launch<128, WNW_PAGES_INT8>(a, map, nt, n_ctas, cluster, pages->device, st);
   }
   if (e != cudaSuccess || cluster) return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
-  const dim3 grid(n_sm, prompt ? 16 : a.rt * a.g);
+  const dim3 grid(n_sm, prompt ? 32 : a.rt * a.g);
   e = pg_launch(d == 64 ? wnw_pages_join_kernel<64> : wnw_pages_join_kernel<128>, grid, 128, 0, st, 0, a);
   return e == cudaSuccess ? WNW_OK : WNW_ERR_CUDA;
 }

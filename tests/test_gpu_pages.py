@@ -192,6 +192,13 @@ def test_write_of_every_bf16_magnitude(fmt):
     b.check()
     b.write(x.flip(0).contiguous(), x, [1] * n)          # a second token: scales rise or stay
     b.check()
+    for dtype in (torch.bfloat16, torch.float16):
+        k, v = (torch.empty(2 * n, 1, 64, dtype=dtype, device=DEV) for _ in range(2))
+        wnw.wnw_pages_read(b.pages, b.table_dev, ints([0] * n), starts_of([2] * n), k, v)
+        want = np.concatenate([b.ref.values(b.table[s], 2) for s in range(n)], axis=1)
+        most = torch.finfo(dtype).max
+        want = torch.tensor(np.clip(want, -most, most)).to(dtype)            # (exact in bf16; one rounding in fp16)
+        assert torch.equal(torch.stack([k, v]).cpu().nan_to_num(nan=1.5), want.nan_to_num(nan=1.5))
 
 
 @pytest.mark.parametrize("fmt", [E4M3, INT8])
