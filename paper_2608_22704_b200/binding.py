@@ -601,7 +601,7 @@ def _batch(page_table, lengths, row_starts, device: int, n_rows: int, max_rows: 
     _ints(row_starts, (n + 1,), what, "row_starts", device)
     if n < 2:
         stride = width
-    if (one != 1 and width > 1) or stride < width or (n > 1 and (lengths.stride(0) != 1 or row_starts.stride(0) != 1)):
+    if (one != 1 and width > 1) or stride < width or not lengths.is_contiguous() or not row_starts.is_contiguous():
         _refuse(what, "page_table, lengths and row_starts: contiguous, sequences apart from one another")
     return page_table.data_ptr(), lengths.data_ptr(), row_starts.data_ptr(), stride, n, n_rows, max_rows
 

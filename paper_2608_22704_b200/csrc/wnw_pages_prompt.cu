@@ -1,9 +1,13 @@
 // wnw_pages_attend for many query rows of a sequence (a prompt, a piece of one): the same formula and the same two references as the kernel
 // for few rows (wnw_pages_attn.cu), on the fifth-generation tensor cores.
 //
-// What bounds it: two products of 128 x 128 x head_dim per tile of 128 tokens and 128 query rows, and one exp2 per score, of which an SM
-// does 16 a clock: 1024 clocks a tile, twice what the products take.  The codes are small beside that, but have to become fp16 in shared
-// memory before the tensor cores can take them; so a CTA works on two tiles of query rows at a time and turns each tile of codes once.
+// What bounds it: two products of 128 x 128 x head_dim per tile of 128 tokens and 128 query rows, 1024 clocks at the tensor cores' rate for a
+// head_dim of 128, and one exp2 per score, of which an SM does 16 a clock: 1024 clocks too.  The codes are few beside that, but have to become
+// fp16 in shared memory before the tensor cores can take them; so a CTA works on two tiles of query rows at a time and turns each tile of codes
+// once.  2049 rows of 32 heads behind 13015 tokens of 8 KV heads take 630 us: 750 TFLOP/s, where a library's large bf16 product reaches 1639.
+// A tile of tokens takes 5250 clocks for the two row tiles, not 2048: each row tile's chain of scores, softmax and values is as long as that
+// (softmax 3500), with two of them side by side, for tensor memory holds no third; Q K^T, both of whose operands come from shared memory, takes 680
+// to 970 clocks instead of 512 beside the other traffic there.
 //
 // 16 warps: 0-3 and 4-7 softmax of the two row tiles (a thread a row), 8-11 codes to fp16, 12 issues the products.
 //   S_i = Q_i K^T         operands in shared memory, 128-byte swizzle, rows of 64 elements; S_i fp32 in tensor memory

@@ -320,7 +320,7 @@ def check_attention(out, lse, q, values, lengths, rows, causal, scale=0.0, T=256
         gone = np.isneginf(want_lse)
         assert np.array_equal(np.isneginf(got_lse), gone) and (got[gone] == 0).all()
         fine = np.isfinite(want_lse)
-        assert (np.abs(got_lse - want_lse)[fine] <= tol_lse[fine]).all(), (s, np.abs(got_lse - want_lse)[fine].max())
+        assert (np.abs(got_lse[fine] - want_lse[fine]) <= tol_lse[fine]).all(), (s, np.abs(got_lse[fine] - want_lse[fine]).max())
         at += r
     assert (out[at:] == 7.0).all() and (lse[at:] == 7.0).all()              # rows behind the last sequence's
 
