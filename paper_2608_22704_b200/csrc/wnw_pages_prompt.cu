@@ -4,9 +4,9 @@
 // What bounds it: two products of 128 x 128 x head_dim per tile of 128 tokens and 128 query rows, 1024 clocks at the tensor cores' rate for a
 // head_dim of 128, and one exp2 per score, of which an SM does 16 a clock: 1024 clocks too.  The codes are few beside that, but have to become
 // fp16 in shared memory before the tensor cores can take them; so a CTA works on two tiles of query rows at a time and turns each tile of codes
-// once.  2049 rows of 32 heads behind 13015 tokens of 8 KV heads take 630 us: 750 TFLOP/s, where a library's large bf16 product reaches 1639.
-// A tile of tokens takes 5250 clocks for the two row tiles, not 2048: each row tile's chain of scores, softmax and values is as long as that
-// (softmax 3500), with two of them side by side, for tensor memory holds no third; Q K^T, both of whose operands come from shared memory, takes 680
+// once.  2049 rows of 32 heads behind 13015 tokens of 8 KV heads take 596 us: 790 TFLOP/s, where a library's large bf16 product reaches 1639.
+// A tile of tokens takes 4900 clocks for the two row tiles, not 2048: each row tile's chain of scores, softmax and values is as long as that
+// (softmax some 3200), with two of them side by side, for tensor memory holds no third; Q K^T, both of whose operands come from shared memory, takes 680
 // to 970 clocks instead of 512 beside the other traffic there.
 //
 // 16 warps: 0-3 and 4-7 softmax of the two row tiles (a thread a row), 8-11 codes to fp16, 12 issues the products.
@@ -141,36 +141,41 @@ __device__ __forceinline__ float upper(uint64_t x) { return __uint_as_float((uin
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
 // The largest score (`top`), and the largest with its V scale (`big`).  seen: of the tile's tokens, by the row.  32 tokens at a time, the
-// next ones on their way meanwhile; x[0] holds the first ones again afterwards.
+// next ones on their way meanwhile; x[0] holds the first ones again afterwards.  (The loops are rolled up to two turns of 32: all 128 laid out
+// crowd the instruction cache and the registers, 631 us instead of 596 where the file's head says 2049 rows.)
 template <bool MASKED>
 __device__ __forceinline__ void row_top(uint32_t t_s, uint32_t (&x)[2][32], const float2 *scale, bool even, float f_row, int seen, float &top, float &big) {
   top = -INFINITY;
   big = NOTHING;
+#pragma unroll 1
+  for (int k0 = 0; k0 < 4; k0 += 2) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    tmem_loaded(x[k & 1]);
-    tmem_load(t_s + 32 * ((k + 1) & 3), x[(k + 1) & 1]);
-    float t[2];
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      float y[16];
-#pragma unroll
-      for (int z = 0; z < 16; ++z) {
-        y[z] = __uint_as_float(x[k & 1][16 * g + z]);
-        if (MASKED && 32 * k + 16 * g + z >= seen) y[z] = -INFINITY;
-      }
-      t[g] = fmaxf(max3(max3(y[0], y[1], y[2]), max3(y[3], y[4], y[5]), max3(y[6], y[7], y[8])),
-                   max3(max3(y[9], y[10], y[11]), max3(y[12], y[13], y[14]), y[15]));
-    }
-    if (!MASKED && even) {
-      top = max3(top, t[0], t[1]);
-    } else {
+    for (int h = 0; h < 2; ++h) {
+      const int k = k0 + h;
+      tmem_loaded(x[h]);
+      tmem_load(t_s + 32 * ((k + 1) & 3), x[h ^ 1]);
+      float t[2];
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        const float2 sc = scale[2 * k + g];
-        const float s = MASKED && (t[g] == -INFINITY || sc.y == -INFINITY) ? -INFINITY : t[g] * (f_row * sc.x);
-        top = fmaxf(top, s);
-        big = fmaxf(big, s + sc.y);
+        float y[16];
+#pragma unroll
+        for (int z = 0; z < 16; ++z) {
+          y[z] = __uint_as_float(x[h][16 * g + z]);
+          if (MASKED && 32 * k + 16 * g + z >= seen) y[z] = -INFINITY;
+        }
+        t[g] = fmaxf(max3(max3(y[0], y[1], y[2]), max3(y[3], y[4], y[5]), max3(y[6], y[7], y[8])),
+                     max3(max3(y[9], y[10], y[11]), max3(y[12], y[13], y[14]), y[15]));
+      }
+      if (!MASKED && even) {
+        top = max3(top, t[0], t[1]);
+      } else {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const float2 sc = scale[2 * k + g];
+          const float s = MASKED && (t[g] == -INFINITY || sc.y == -INFINITY) ? -INFINITY : t[g] * (f_row * sc.x);
+          top = fmaxf(top, s);
+          big = fmaxf(big, s + sc.y);
+        }
       }
     }
   }
@@ -184,32 +189,36 @@ __device__ __forceinline__ void row_top(uint32_t t_s, uint32_t (&x)[2][32], cons
 // zeros beside one of large values), d is 60 there and the rest a factor of its own (DEEP).  P's columns lie where S has been read.
 template <bool MASKED, bool DEEP>
 __device__ __forceinline__ void row_weights(uint32_t t_s, uint32_t (&x)[2][32], const float2 *scale, float f_row, int seen, float m, float big_m, float &l) {
+#pragma unroll 1
+  for (int k0 = 0; k0 < 4; k0 += 2) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    tmem_loaded(x[k & 1]);
-    if (k < 3) tmem_load(t_s + 32 * (k + 1), x[(k + 1) & 1]);
-    uint32_t p[16];
+    for (int h = 0; h < 2; ++h) {
+      const int k = k0 + h;
+      tmem_loaded(x[h]);
+      if (k < 3) tmem_load(t_s + 32 * (k + 1), x[h ^ 1]);
+      uint32_t p[16];
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const float2 sc = scale[2 * k + g];
-      const bool hole = MASKED && sc.y == -INFINITY;
-      const int lim = hole ? 0 : seen;
-      const float f = f_row * sc.x, d = hole ? 0.f : big_m - sc.y - m, d2 = DEEP ? fminf(d, 60.f) : d, off = -(m + d2), rest = DEEP ? ex2(d2 - d) : 1.f;
-      const uint64_t ff = two(f, f), oo = two(off, off);
-      uint64_t sum[2] = {0, 0};
+      for (int g = 0; g < 2; ++g) {
+        const float2 sc = scale[2 * k + g];
+        const bool hole = MASKED && sc.y == -INFINITY;
+        const int lim = hole ? 0 : seen;
+        const float f = f_row * sc.x, d = hole ? 0.f : big_m - sc.y - m, d2 = DEEP ? fminf(d, 60.f) : d, off = -(m + d2), rest = DEEP ? ex2(d2 - d) : 1.f;
+        const uint64_t ff = two(f, f), oo = two(off, off);
+        uint64_t sum[2] = {0, 0};
 #pragma unroll
-      for (int z = 0; z < 16; z += 2) {
-        const uint64_t y = fma2(two(__uint_as_float(x[k & 1][16 * g + z]), __uint_as_float(x[k & 1][16 * g + z + 1])), ff, oo);
-        float u = ex2(lower(y)), v = ex2(upper(y));
-        if (MASKED && 32 * k + 16 * g + z >= lim) u = 0.f;
-        if (MASKED && 32 * k + 16 * g + z + 1 >= lim) v = 0.f;
-        sum[z >> 1 & 1] = add2(sum[z >> 1 & 1], two(u, v));
-        p[8 * g + z / 2] = DEEP ? half2_of(u * rest, v * rest) : half2_of(u, v);
+        for (int z = 0; z < 16; z += 2) {
+          const uint64_t y = fma2(two(__uint_as_float(x[h][16 * g + z]), __uint_as_float(x[h][16 * g + z + 1])), ff, oo);
+          float u = ex2(lower(y)), v = ex2(upper(y));
+          if (MASKED && 32 * k + 16 * g + z >= lim) u = 0.f;
+          if (MASKED && 32 * k + 16 * g + z + 1 >= lim) v = 0.f;
+          sum[z >> 1 & 1] = add2(sum[z >> 1 & 1], two(u, v));
+          p[8 * g + z / 2] = DEEP ? half2_of(u * rest, v * rest) : half2_of(u, v);
+        }
+        const uint64_t both = add2(sum[0], sum[1]);
+        l = __fmaf_rn(lower(both) + upper(both), ex2(d2), l);
       }
-      const uint64_t both = add2(sum[0], sum[1]);
-      l = __fmaf_rn(lower(both) + upper(both), ex2(d2), l);
+      tmem_store(t_s + 16 * k, p);
     }
-    tmem_store(t_s + 16 * k, p);
   }
 }
 
