@@ -18,6 +18,9 @@
 // The scales 2^eV sit inside the sum over tokens.  A second reference M, the maximum of s + eV in log2, carries them: weights enter the
 // product as 2^(s + eV - M), the denominator as 2^(s - m), and out = product * 2^(M - m) / denominator.  No spread of scales over the
 // pages can push the weights that matter out of fp16's range.
+//
+// 16 sequences of 50001 tokens, 8 KV heads of 128, e4m3: 248 us, 6.6 TB/s (the measured copy rate is 6.5).  Some 10 us of a call on the line go
+// into laying it out, its first copies, and the join: 32 sequences of up to 7500 tokens, int8, 332 MB, take 74 us.
 #include <cuda.h>
 
 #include <algorithm>
@@ -29,7 +32,7 @@
 namespace wnw {
 namespace {
 
-constexpr int PA_ROWS = 16;           // query rows of an item at most
+constexpr int PA_ROWS = 16;          // query rows of an item at most
 constexpr int PA_SEGS = 64;          // stretches of heads that a CTA prepares at a time
 
 // A head's stretch inside a CTA.
@@ -232,35 +235,33 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
       n_seg = 1;
       ++item0;
     } else {
-      {
-          int mine = 0;
-        if (tid < PA_SEGS && item0 + tid < n_items) {
-          const int item = item0 + tid;
-          int lo = 0, hi = a.bv.n_seqs;
-          while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (items[mid] <= item) lo = mid; else hi = mid; }
-            const int cap = a.bv.stride * pv.T, r0 = max(a.bv.starts[lo], 0), n = max(0, min(a.bv.starts[lo + 1], a.bv.n_rows) - r0);
-          const int len = max(0, min(a.bv.lengths[lo], cap)), tiles = n <= a.rt ? 1 : (n + a.rt - 1) / a.rt, it = item - items[lo];
-          const int per = max(1, (len + PG_GR - 1) / PG_GR);
-          const long long b = grans[lo] + (long long)it * per, e = b + per;
-          if (b < x1) {
-            mine = 1;
-            Seg &sg = segs[tid];
-            const long long f = max(b, x0), l = min(e, x1);
-            sg.s = lo; sg.h = tiles == 1 ? it : it / tiles; sg.tile = tiles == 1 ? 0 : it % tiles;
-            sg.g0 = (int)(f - b); sg.n = (int)(l - f); sg.y0 = (int)(f - x0);
-            sg.len = len;
-            sg.r0 = r0; sg.n_seq = n;
-            sg.nq = min(a.rt, n - sg.tile * a.rt);
-            sg.row0 = r0 + sg.tile * a.rt;
-            sg.end0 = a.causal ? len - n + sg.tile * a.rt + 1 : len;
-            const int last = min(len, a.causal ? sg.end0 + sg.nq - 1 : len);
-            sg.need = last > 0 ? (last + PG_GR - 1) / PG_GR : 0;
-            sg.slot = b >= x0 && e <= x1 ? -1 : b < x0 ? 0 : 1;
-            sg.n_parts = sg.slot == 1 ? (int)quotient(e - 1 - x0, len_line) + 1 : 0;
-          }
+      int mine = 0;
+      if (tid < PA_SEGS && item0 + tid < n_items) {
+        const int item = item0 + tid;
+        int lo = 0, hi = a.bv.n_seqs;
+        while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (items[mid] <= item) lo = mid; else hi = mid; }
+        const int cap = a.bv.stride * pv.T, r0 = max(a.bv.starts[lo], 0), n = max(0, min(a.bv.starts[lo + 1], a.bv.n_rows) - r0);
+        const int len = max(0, min(a.bv.lengths[lo], cap)), tiles = n <= a.rt ? 1 : (n + a.rt - 1) / a.rt, it = item - items[lo];
+        const int per = max(1, (len + PG_GR - 1) / PG_GR);
+        const long long b = grans[lo] + (long long)it * per, e = b + per;
+        if (b < x1) {
+          mine = 1;
+          Seg &sg = segs[tid];
+          const long long f = max(b, x0), l = min(e, x1);
+          sg.s = lo; sg.h = tiles == 1 ? it : it / tiles; sg.tile = tiles == 1 ? 0 : it % tiles;
+          sg.g0 = (int)(f - b); sg.n = (int)(l - f); sg.y0 = (int)(f - x0);
+          sg.len = len;
+          sg.r0 = r0; sg.n_seq = n;
+          sg.nq = min(a.rt, n - sg.tile * a.rt);
+          sg.row0 = r0 + sg.tile * a.rt;
+          sg.end0 = a.causal ? len - n + sg.tile * a.rt + 1 : len;
+          const int last = min(len, a.causal ? sg.end0 + sg.nq - 1 : len);
+          sg.need = last > 0 ? (last + PG_GR - 1) / PG_GR : 0;
+          sg.slot = b >= x0 && e <= x1 ? -1 : b < x0 ? 0 : 1;
+          sg.n_parts = sg.slot == 1 ? (int)quotient(e - 1 - x0, len_line) + 1 : 0;
         }
-        n_seg = __syncthreads_count(mine);
       }
+      n_seg = __syncthreads_count(mine);
       more = n_seg == PA_SEGS;                          // (a last round of none costs nothing)
       item0 += n_seg;
     }
