@@ -469,8 +469,8 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
 #pragma unroll
               for (int z = 0; z < G::VB / 4; ++z) vw[t][z] = 0;
         }
-        bool nan_codes = false;                          // in a granule that some rows see only part of
-        if (FMT == WNW_PAGES_E4M3 && partly && a.causal && sg.nq > 1) {
+        bool nan_codes = false;                          // in a granule that some rows see only part of: a tile of one row too, before the sequence's others
+        if (FMT == WNW_PAGES_E4M3 && partly && end_min < sg.len) {
           bool mine = false;
 #pragma unroll
           for (int t = 0; t < 4; ++t)
