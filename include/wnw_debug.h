@@ -47,6 +47,24 @@ typedef enum {
 } wnw_debug_cut_t;
 wnw_status_t wnw_debug_get_layer_cut(wnw_cache_t *cache, int32_t layer, int32_t cut[3]);
 
+/* Test hook for wnw_pages_attend's bounded waits: in the calls of the process that follow (captured ones as they are captured), waits of
+ * these kinds are for something that never happens, and waits give up after 2^20 SM clocks.  A CTA whose wait runs out touches nothing of
+ * what stands behind it, sets WNW_PAGES_TIMEOUT in the store's status word, lets what it has under way finish and writes not-a-numbers
+ * to the rows that it has not finished.  0: none, as at the start.  Not for production use. */
+typedef enum {
+  WNW_DEBUG_WAIT_K_FREE = 1,     /* of many rows: room for a tile of K as fp16 */
+  WNW_DEBUG_WAIT_V_FREE = 2,     /* ... of V */
+  WNW_DEBUG_WAIT_K_FULL = 4,     /* ... a tile of K */
+  WNW_DEBUG_WAIT_V_FULL = 8,     /* ... of V */
+  WNW_DEBUG_WAIT_Q_FULL = 16,    /* ... the query rows */
+  WNW_DEBUG_WAIT_SCORES = 32,    /* ... Q K^T */
+  WNW_DEBUG_WAIT_WEIGHTS = 64,   /* ... the softmax */
+  WNW_DEBUG_WAIT_VALUES = 128,   /* ... P V */
+  WNW_DEBUG_WAIT_BEGUN = 256,    /* ... the start of a segment that has no rows for one of the two row tiles */
+  WNW_DEBUG_WAIT_ALL = 511
+} wnw_debug_wait_t;
+wnw_status_t wnw_debug_pages_lose(int32_t waits);
+
 /* Optional per-kernel timing: when enabled the library brackets its attention-kernel launches with CUDA events
  * on the launching stream; wnw_get_kernel_time returns the accumulated milliseconds and launch count since the
  * last call (drains the stream).  Off by default. */

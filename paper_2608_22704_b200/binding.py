@@ -28,6 +28,9 @@ WNW_TIDAL_KV_BF16, WNW_TIDAL_KV_FP8_E4M3 = 0, 1
 WNW_DTYPE_BF16, WNW_DTYPE_FP16, WNW_DTYPE_FP32 = 0, 1, 2
 WNW_PAGES_E4M3, WNW_PAGES_INT8 = 0, 1
 WNW_PAGES_BAD_PAGE, WNW_PAGES_BAD_LENGTH, WNW_PAGES_TIMEOUT = 1, 2, 4
+(WNW_DEBUG_WAIT_K_FREE, WNW_DEBUG_WAIT_V_FREE, WNW_DEBUG_WAIT_K_FULL, WNW_DEBUG_WAIT_V_FULL, WNW_DEBUG_WAIT_Q_FULL, WNW_DEBUG_WAIT_SCORES,
+ WNW_DEBUG_WAIT_WEIGHTS, WNW_DEBUG_WAIT_VALUES, WNW_DEBUG_WAIT_BEGUN) = (1 << i for i in range(9))
+WNW_DEBUG_WAIT_ALL = 511
 
 
 class wnw_config_t(C.Structure):
@@ -133,6 +136,7 @@ _SIGNATURES = {
     "wnw_debug_attend_static_cluster": [_i32, _i32, _i32, _i32, _i32, C.POINTER(_i32)],
     "wnw_attend_static": [_vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32, C.c_float, _i32, _vp],
     "wnw_attend_static_status": [_i32, _vp, C.POINTER(_i32)],
+    "wnw_debug_pages_lose": [_i32],
     "wnw_rotary_init": [C.POINTER(wnw_rotary_t), _i32, C.c_double, C.POINTER(_i32), _i32, _i32, _i32],
     "wnw_rotate": [_vp],
     "wnw_pages_write": [_vp],
@@ -646,6 +650,11 @@ def wnw_pages_attend_workspace(pages, n_q_heads: int) -> int:
     n = C.c_int64()
     _ck(lib().wnw_pages_attend_workspace(C.byref(pages), n_q_heads, C.byref(n)), "wnw_pages_attend_workspace")
     return n.value
+
+
+def wnw_debug_pages_lose(waits: int) -> None:
+    """Test hook: waits of these kinds (WNW_DEBUG_WAIT_*) run out in the calls of wnw_pages_attend that follow."""
+    _ck(lib().wnw_debug_pages_lose(waits), "wnw_debug_pages_lose")
 
 
 def wnw_pages_attend(pages, page_table, lengths, row_starts, q, out, workspace, lse=None, causal=True, softmax_scale=0.0, max_rows=0,

@@ -798,6 +798,8 @@ int cluster_of(const AttendArgs &a, int tiles, int d, int n_sm) {
   return c && (long long)a.bv.stride * a.pv.T * 2 * d * tiles <= c * CLUSTER_BYTES ? c : 0;
 }
 
+std::atomic<int> lose{0};            // of the calls to come
+
 wnw_status_t check_heads(const wnw_pages_t *p, int n_q_heads) {
   if (n_q_heads < 1 || n_q_heads % p->n_kv_heads) return WNW_ERR_INVALID_ARG;
   return n_q_heads / p->n_kv_heads > 16 ? WNW_ERR_UNSUPPORTED : WNW_OK;
@@ -818,6 +820,12 @@ extern "C" wnw_status_t wnw_pages_attend_workspace(const wnw_pages_t *pages, int
   if (!on.ok || pg_sms(pages->device, &n_sm) != WNW_OK) return WNW_ERR_CUDA;
   size_t r, h;
   *bytes = (int64_t)workspace_bytes(n_sm, pages->head_dim, &r, &h);
+  return WNW_OK;
+}
+
+extern "C" wnw_status_t wnw_debug_pages_lose(int32_t waits) {
+  if (waits & ~WNW_DEBUG_WAIT_ALL) return WNW_ERR_INVALID_ARG;
+  lose.store(waits, std::memory_order_relaxed);
   return WNW_OK;
 }
 
@@ -851,6 +859,9 @@ extern "C" wnw_status_t wnw_pages_attend(const wnw_pages_attend_t *call) {
   a.g = q.n_heads / pages->n_kv_heads;
   a.dtype = dtype;
   a.causal = call->causal;
+  a.lose = lose.load(std::memory_order_relaxed);
+  a.wait_clocks = a.lose ? 1 << 20 : PP_WAIT_CLOCKS;
+  a.values_parity = a.lose & WNW_DEBUG_WAIT_VALUES ? 0 : 1;
   a.scale_log2 = (float)((softmax_scale > 0.f ? (double)softmax_scale : 1.0 / std::sqrt((double)pages->head_dim)) * 1.4426950408889634);
   a.part_o = (float *)workspace_dev;
   a.part_row = (PartRow *)((char *)workspace_dev + rows_at);

@@ -1,5 +1,6 @@
 // What the attention kernels over the paged store share: arguments, partial results of heads that several CTAs work on, codes as fp16.
 #pragma once
+#include "../../include/wnw_debug.h"
 #include "wnw_pages.cuh"
 
 namespace wnw {
@@ -20,6 +21,9 @@ struct AttendArgs {
   float *lse;
   int Hq, g, rt, rb, blocks;
   int dtype, causal;
+  int lose;                          // WNW_DEBUG_WAIT_*: waits that are to run out
+  uint32_t values_parity;            // 1; 0 where the waits for P V are to run out: not every tile has one, and of a phase that never ends the odd ones are over
+  uint32_t wait_clocks;              // after which a wait gives up
   float scale_log2;
   float *part_o;                     // [CTA][2][blocks * rb][D]
   PartRow *part_row;                 // [CTA][2][blocks * rb]
@@ -64,6 +68,7 @@ __device__ __forceinline__ long long quotient(long long x, long long y) {
 
 // The attention of many query rows (wnw_pages_prompt.cu): 128-row tiles, two at a time.
 constexpr int PP_ROWS = 128, PP_BLOCKS = 2;
+constexpr uint32_t PP_WAIT_CLOCKS = 2000000000;
 cudaError_t launch_prompt(const AttendArgs &a, int head_dim, int format, int n_ctas, int device, cudaStream_t st);
 
 }  // namespace wnw

@@ -4,12 +4,12 @@
 // What bounds it: two products of 128 x 128 x head_dim per tile of 128 tokens and 128 query rows, 1024 clocks at the tensor cores' rate for a
 // head_dim of 128, and one exp2 per score, of which an SM does 16 a clock: 1024 clocks too.  The codes are few beside that, but have to become
 // fp16 in shared memory before the tensor cores can take them; so a CTA works on two tiles of query rows at a time and turns each tile of codes
-// once.  2049 rows of 32 heads behind 13015 tokens of 8 KV heads take 596 us: 790 TFLOP/s, where a library's large bf16 product reaches 1639.
+// once.  2049 rows of 32 heads behind 13015 tokens of 8 KV heads take 607 us: 776 TFLOP/s, where a library's large bf16 product reaches 1639.
 // A tile of tokens takes 4900 clocks for the two row tiles, not 2048: each row tile's chain of scores, softmax and values is as long as that
 // (softmax some 3200), with two of them side by side, for tensor memory holds no third; Q K^T, both of whose operands come from shared memory, takes 680
 // to 970 clocks instead of 512 beside the other traffic there.
 //
-// 16 warps: 0-3 and 4-7 softmax of the two row tiles (a thread a row), 8-11 codes to fp16, 12 issues the products.
+// 16 warps: 0-3 and 4-7 softmax of the two row tiles (a thread a row), 8-11 codes to fp16, 12 issues the products, 13 has the tensor memory.
 //   S_i = Q_i K^T         operands in shared memory, 128-byte swizzle, rows of 64 elements; S_i fp32 in tensor memory
 //   O_i += P_i V          P_i (fp16) in tensor memory over S_i, V as it lies (its rows are the contracted index)
 // Tensor memory: S_0 S_1 O_0 O_1, 128 columns each.  While the products of one row tile run, the other's softmax does.
@@ -43,7 +43,7 @@ struct Walk {
 struct Shared {
   uint64_t k_full[2], k_free[2], v_full[2], v_free[2], q_full[2], s_full[2], p_ready[2], o_done[2], begun;
   uint32_t tmem;
-  int dead;                          // a wait ran out: nobody waits any more
+  uint32_t dead;                     // a wait ran out: nobody waits any more, and no product is issued
   float2 scale[4][8];                // per tile and granule: 2^eK, eV; eV = -inf: the granule is not there
   uint32_t flags[4];                 // TILE_* below
   // Not-a-numbers among the V codes, per warp that turns codes (each keeps its own), four segments deep (a slot is used again when the
@@ -51,32 +51,41 @@ struct Shared {
   int nan_any[4][4], nan_first[4][4][128];
   long long sums[17];
   long long line[PG_MAX_SEQS + 1];   // tiles before each sequence
+  uint64_t drained;                  // the products are done, and no more come
+  int32_t *status;
+  uint32_t clocks;                   // after which a wait gives up
 };
 template <int D> constexpr size_t tiles_bytes() { return 8 * 128 * D * 2 / 4 * 3; }   // 2 Q + 2 K + 2 V of 128 rows
 template <int D> constexpr size_t smem_bytes() { return tiles_bytes<D>() + sizeof(Shared) + 1024; }
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(smem_u32(bar)) : "memory"); }
-// Bounded: after about a second of SM clocks the CTA gives up for good, and says so.
-__device__ __noinline__ void wait_long(uint32_t bar, uint32_t parity, volatile int *dead, int32_t *status) {
-  const long long t0 = clock64();
-  while (!try_wait(bar, parity)) {
-    if (*dead) return;
-    if (clock64() - t0 > 2000000000ll) {
-      *dead = 1;
-      if (status) atomicOr(status, WNW_PAGES_TIMEOUT);
-      return;
-    }
-  }
-}
-__device__ __forceinline__ void wait(uint64_t *bar, uint32_t parity, Shared &sh, const PagesView &pv) {
-  if (!try_wait(smem_u32(bar), parity & 1)) wait_long(smem_u32(bar), parity & 1, &sh.dead, pv.status);
-}
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory"); }
 __device__ __forceinline__ void fence_smem() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }
-__device__ __forceinline__ void commit(uint64_t *bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(smem_u32(bar)) : "memory");
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t *bar) { commit(smem_u32(bar)); }
+// Bounded waits.  After about a second of SM clocks the CTA gives up for good, and says so: the thread of the products (PRODUCTS) waits for
+// those under way and ends; the other warps wait for that, so that nothing they touch is in use, and then go on without waiting; their rows
+// become not-a-numbers where they are put out.  All of it lies out of the way of a wait that ends: as branches behind the waits it made 607 us
+// 618 where the file's head says 2049 rows.
+template <bool PRODUCTS> __device__ __noinline__ void wait_long(uint32_t bar, uint32_t parity, volatile Shared *sh) {
+  const long long t0 = clock64();
+  while (!try_wait(bar, parity)) {
+    if (!sh->dead && clock64() - t0 <= sh->clocks) continue;
+    if (!sh->dead && sh->status) atomicOr(sh->status, WNW_PAGES_TIMEOUT);
+    sh->dead = 1;
+    const uint32_t drained = smem_u32((const void *)&sh->drained);
+    if (PRODUCTS) commit(drained);
+    for (const long long t1 = clock64(); !try_wait(drained, 0) && clock64() - t1 <= PP_WAIT_CLOCKS;) {}
+    if (PRODUCTS) asm volatile("exit;\n");
+    return;
+  }
+}
+template <bool PRODUCTS = false> __device__ __forceinline__ void wait(uint64_t *bar, uint32_t parity, Shared &sh) {
+  if (!try_wait(smem_u32(bar), parity & 1)) wait_long<PRODUCTS>(smem_u32(bar), parity & 1, &sh);
 }
 // Operands of 128-byte rows in the 128-byte swizzle, eight rows an atom.  lbo: from 64 elements of the outer index to the next 64, where that
 // is the contiguous one (V); not used otherwise.
@@ -142,7 +151,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(
 
 // The largest score (`top`), and the largest with its V scale (`big`).  seen: of the tile's tokens, by the row.  32 tokens at a time, the
 // next ones on their way meanwhile; x[0] holds the first ones again afterwards.  (The loops are rolled up to two turns of 32: all 128 laid out
-// crowd the instruction cache and the registers, 631 us instead of 596 where the file's head says 2049 rows.)
+// crowd the instruction cache and the registers, 631 us instead of 596 when it was done, where the file's head says 2049 rows.)
 template <bool MASKED>
 __device__ __forceinline__ void row_top(uint32_t t_s, uint32_t (&x)[2][32], const float2 *scale, bool even, float f_row, int seen, float &top, float &big) {
   top = -INFINITY;
@@ -351,12 +360,24 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
   const PagesView &pv = a.pv;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   if (tid == 0) {
+    auto init = [&](uint64_t *bar, int count, int kind) {   // (for arrivals that nothing makes, where a test asks for waits that run out)
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(smem_u32(bar)), "r"(count + (a.lose & kind ? 1 << 16 : 0)) : "memory");
+    };
     for (int i = 0; i < 2; ++i) {
-      for (uint64_t *b : {&sh.k_full[i], &sh.v_full[i], &sh.q_full[i], &sh.p_ready[i]}) asm volatile("mbarrier.init.shared::cta.b64 [%0], 4;\n" ::"r"(smem_u32(b)) : "memory");
-      for (uint64_t *b : {&sh.k_free[i], &sh.v_free[i], &sh.s_full[i], &sh.o_done[i]}) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;\n" ::"r"(smem_u32(b)) : "memory");
+      init(&sh.k_full[i], 4, WNW_DEBUG_WAIT_K_FULL);
+      init(&sh.v_full[i], 4, WNW_DEBUG_WAIT_V_FULL);
+      init(&sh.q_full[i], 4, WNW_DEBUG_WAIT_Q_FULL);
+      init(&sh.p_ready[i], 4, WNW_DEBUG_WAIT_WEIGHTS);
+      init(&sh.k_free[i], 1, WNW_DEBUG_WAIT_K_FREE);
+      init(&sh.v_free[i], 1, WNW_DEBUG_WAIT_V_FREE);
+      init(&sh.s_full[i], 1, WNW_DEBUG_WAIT_SCORES);
+      init(&sh.o_done[i], 1, WNW_DEBUG_WAIT_VALUES);
     }
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;\n" ::"r"(smem_u32(&sh.begun)) : "memory");
+    init(&sh.begun, 1, WNW_DEBUG_WAIT_BEGUN);
+    init(&sh.drained, 1, 0);
     fence_smem();
+    sh.status = pv.status;
+    sh.clocks = a.wait_clocks;
     sh.dead = 0;
   }
   pg_let_next_start();
@@ -365,7 +386,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
   const long long total = lay_out(a, sh);              // (its barriers order the above too)
   const long long len_line = (total + gridDim.x - 1) / gridDim.x, x0 = min(total, blockIdx.x * len_line), x1 = min(total, x0 + len_line);
   if (x0 >= x1) return;
-  if (wid == 12) {
+  if (wid == 13) {                                     // (the warp that frees it has to be whole: 12 may have lost the thread of the products)
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(&sh.tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     fence_before();
@@ -389,7 +410,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
         n_all += n_tiles;
         __syncwarp();
         if (lane == 0) arrive(&sh.q_full[1]);
-        wait(&sh.begun, n_idle++, sh, pv);
+        wait(&sh.begun, n_idle++, sh);
         continue;
       }
       const int first = (w.t * PP_BLOCKS + i) * a.rt, tok = first + tok_in;
@@ -432,7 +453,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
       const int end = real ? min(w.len, a.causal ? w.len - w.n + tok + 1 : w.len) : w.len;
       float m = NOTHING, big_m = NOTHING, l = 0.f;
       for (int kt = w.k0; kt < w.k1; ++kt, ++n_all, ++n_mine) {
-        wait(&sh.s_full[i], n_mine, sh, pv);
+        wait(&sh.s_full[i], n_mine, sh);
         fence_after();
         const float2 *scale = sh.scale[n_all & 3];
         const uint32_t flags = sh.flags[n_all & 3];
@@ -449,7 +470,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
           m = mn;
           big_m = bn;
           if (kt > w.k0) {
-            wait(&sh.o_done[i], n_mine - 1, sh, pv);
+            wait(&sh.o_done[i], (n_mine - 1) & a.values_parity, sh);
             fence_after();
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
@@ -479,8 +500,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
       }
 
       // ---- out ----
-      if (*(volatile int *)&sh.dead) l = NAN;          // incomplete, and looks it
-      wait(&sh.o_done[i], n_mine - 1, sh, pv);
+      wait(&sh.o_done[i], (n_mine - 1) & a.values_parity, sh);
+      if (*(volatile uint32_t *)&sh.dead) l = NAN;     // incomplete, and looks it (read last: this wait, too, or another warp's may have run out)
       fence_after();
       const bool whole = w.k0 == 0 && w.k1 == w.need;
       const int slot = w.k0 ? 0 : 1;
@@ -599,7 +620,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
         const uint32_t meta = c.meta;
         const uint32_t meta_0 = __shfl_sync(0xffffffffu, meta, 0);
         const bool even = __all_sync(0xffffffffu, lane >= 8 || meta == meta_0), holes = __any_sync(0xffffffffu, lane < 8 && !meta);
-        wait(&sh.k_free[st], (n >> 1) + 1, sh, pv);
+        wait(&sh.k_free[st], (n >> 1) + 1, sh);
         if (wq == 0) {
           if (lane < 8) sh.scale[n & 3][lane] = make_float2(__uint_as_float((meta & 255) << 23), meta ? (float)((int)(meta >> 8 & 255) - 127) : -INFINITY);
           if (lane == 0) sh.flags[n & 3] = (even ? TILE_EVEN : 0) | (holes ? TILE_HOLES : 0);
@@ -619,7 +640,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
         if (lane == 0) arrive(&sh.k_full[st]);
         ask_meta();                                    // (of the next tile: page ids were asked for a tile ago)
         ask(c.k, 0);
-        wait(&sh.v_free[st], (n >> 1) + 1, sh, pv);
+        wait(&sh.v_free[st], (n >> 1) + 1, sh);
         if (FMT == WNW_PAGES_E4M3) {                   // 0x7f and 0xff
           uint32_t any = 0;
 #pragma unroll
@@ -683,9 +704,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
       };
       for (bool more = true; more; more = walk_on(a, w), ++n_seg) {
         const bool two = two_blocks(a, w);
-        wait(&sh.k_full[n & 1], n >> 1, sh, pv);
+        wait<true>(&sh.k_full[n & 1], n >> 1, sh);
         for (int i = 0; i < 2; ++i) {
-          wait(&sh.q_full[i], n_seg, sh, pv);
+          wait<true>(&sh.q_full[i], n_seg, sh);
           fence_after();
           if (i == 0 || two) scores(i, n & 1);
         }
@@ -694,13 +715,13 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
         for (int kt = w.k0; kt < w.k1; ++kt, ++n) {
           const int st = n & 1;
           const bool again = kt + 1 < w.k1;
-          wait(&sh.v_full[st], n >> 1, sh, pv);
+          wait<true>(&sh.v_full[st], n >> 1, sh);
           for (int i = 0; i < (two ? 2 : 1); ++i) {
-            wait(&sh.p_ready[i], n_of[i]++, sh, pv);
+            wait<true>(&sh.p_ready[i], n_of[i]++, sh);
             fence_after();
             values(i, st, kt > w.k0);
             if (again) {
-              if (i == 0) wait(&sh.k_full[st ^ 1], (n + 1) >> 1, sh, pv);
+              if (i == 0) wait<true>(&sh.k_full[st ^ 1], (n + 1) >> 1, sh);
               scores(i, st ^ 1);
             }
           }
@@ -708,12 +729,14 @@ __global__ void __launch_bounds__(PP_THREADS, 1) wnw_pages_prompt_kernel(const _
           if (again) commit(&sh.k_free[st ^ 1]);
         }
       }
+      commit(&sh.drained);
+      wait(&sh.drained, 0, sh);
     }
   }
-  __syncwarp();
+  if (wid != 12) __syncwarp();
   fence_before();
   __syncthreads();
-  if (wid == 12) {
+  if (wid == 13) {
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
   }
