@@ -61,7 +61,8 @@ typedef enum {
   WNW_DEBUG_WAIT_WEIGHTS = 64,   /* ... the softmax */
   WNW_DEBUG_WAIT_VALUES = 128,   /* ... P V */
   WNW_DEBUG_WAIT_BEGUN = 256,    /* ... the start of a segment that has no rows for one of the two row tiles */
-  WNW_DEBUG_WAIT_ALL = 511
+  WNW_DEBUG_WAIT_GRANULE = 512,  /* of few rows: a copy of 16 tokens */
+  WNW_DEBUG_WAIT_ALL = 1023
 } wnw_debug_wait_t;
 wnw_status_t wnw_debug_pages_lose(int32_t waits);
 

@@ -29,8 +29,8 @@ WNW_DTYPE_BF16, WNW_DTYPE_FP16, WNW_DTYPE_FP32 = 0, 1, 2
 WNW_PAGES_E4M3, WNW_PAGES_INT8 = 0, 1
 WNW_PAGES_BAD_PAGE, WNW_PAGES_BAD_LENGTH, WNW_PAGES_TIMEOUT = 1, 2, 4
 (WNW_DEBUG_WAIT_K_FREE, WNW_DEBUG_WAIT_V_FREE, WNW_DEBUG_WAIT_K_FULL, WNW_DEBUG_WAIT_V_FULL, WNW_DEBUG_WAIT_Q_FULL, WNW_DEBUG_WAIT_SCORES,
- WNW_DEBUG_WAIT_WEIGHTS, WNW_DEBUG_WAIT_VALUES, WNW_DEBUG_WAIT_BEGUN) = (1 << i for i in range(9))
-WNW_DEBUG_WAIT_ALL = 511
+ WNW_DEBUG_WAIT_WEIGHTS, WNW_DEBUG_WAIT_VALUES, WNW_DEBUG_WAIT_BEGUN, WNW_DEBUG_WAIT_GRANULE) = (1 << i for i in range(10))
+WNW_DEBUG_WAIT_ALL = 1023
 
 
 class wnw_config_t(C.Structure):

@@ -69,11 +69,11 @@ __device__ __forceinline__ void copy_granule(uint32_t dst, const CUtensorMap *ma
                ::"r"(dst), "l"(map), "r"(bar), "r"(0), "r"(row), "r"(block), "r"(page) : "memory");
 }
 // Bounded: gives up after about a second of SM clocks and says so, instead of hanging.
-__device__ __forceinline__ bool wait_granule(uint32_t bar, uint32_t parity, const PagesView &pv) {
+__device__ __forceinline__ bool wait_granule(uint32_t bar, uint32_t parity, const AttendArgs &a) {
   if (try_wait(bar, parity)) return true;
   const long long t0 = clock64();
   while (!try_wait(bar, parity))
-    if (clock64() - t0 > 2000000000ll) { pg_report(pv, WNW_PAGES_TIMEOUT); return false; }
+    if (clock64() - t0 > a.wait_clocks) { pg_report(a.pv, WNW_PAGES_TIMEOUT); return false; }
   return true;
 }
 
@@ -166,7 +166,8 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, c = lane & 3, r = lane >> 2;
   const int gpp = pv.T / PG_GR;
   if (lane == 0) {
-    for (int k = 0; k < S; ++k) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;\n" ::"r"((uint32_t)__cvta_generic_to_shared(bars + w * S + k)) : "memory");
+    const uint32_t count = a.lose & WNW_DEBUG_WAIT_GRANULE ? 2 : 1;     // (an arrival that nothing makes, where a test asks for copies that do not arrive)
+    for (int k = 0; k < S; ++k) asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"((uint32_t)__cvta_generic_to_shared(bars + w * S + k)), "r"(count) : "memory");
     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
     asm volatile("prefetch.tensormap [%0];\n" ::"l"(&map) : "memory");
   }
@@ -202,6 +203,7 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
   for (int k = 0; k < 2; ++k) v_at[k] = D == 128 ? 16 * (r ^ (2 * c + k)) : 16 * ((r >> 1) ^ c) + 8 * (r & 1);
   const uint32_t ring_u = (uint32_t)__cvta_generic_to_shared(ring) + w * S * G::STAGE, bars_u = (uint32_t)__cvta_generic_to_shared(bars + w * S);
   uint32_t phases = 0;                                  // parity of each stage's next copy
+  bool lost = false;                                    // a copy did not arrive: the warp asks for no more, and what it has a part in is not a number
 
   for (bool more = true; more;) {
     // ---- the next stretches ----
@@ -267,7 +269,7 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
     }
 
     // ---- copies run ahead of the products by S - 1 granules, over the stretches' ends ----
-    int p_seg = -1, p_g = 0, p_end = 0, p_cnt = 0, p_stage = 0;
+    int p_seg = lost ? n_seg : -1, p_g = 0, p_end = 0, p_cnt = 0, p_stage = 0;
     int p_page = 0, p_row = 0;                          // lane i: where the stretch's granule 32 * k + i of this warp is,
     uint32_t p_scale = 0;                               //   exponent fields of its scales, K | V << 8 | 1 << 16 where it is there
     auto fetch = [&]() {
@@ -379,14 +381,23 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
       float e_last = 0.f;
 
       const int g_end = min(sg.g0 + sg.n, sg.need);
-      for (int g = sg.g0 + (w + W - sg.y0 % W) % W; g < g_end; g += W) {
+      for (int g = sg.g0 + (w + W - sg.y0 % W) % W; g < g_end && !lost; g += W) {
         __syncwarp();
         fetch();
         __syncwarp();
         const uint32_t sc = ring_scale[w * S + stage];
         const unsigned char *src = ring + (w * S + stage) * G::STAGE;
         if (sc) {
-          if (!wait_granule(bars_u + 8 * stage, phases >> stage & 1, pv)) l[0][0] = l[0][1] = l[NT - 1][0] = l[NT - 1][1] = NAN;   // incomplete, and looks it
+          if (__any_sync(0xffffffffu, !wait_granule(bars_u + 8 * stage, phases >> stage & 1, a))) {
+            int k = stage;                               // the copies under way, which nothing may disturb, come to rest
+            do {
+              if (ring_scale[w * S + k]) wait_granule(bars_u + 8 * k, phases >> k & 1, a);
+              if (++k == S) k = 0;
+            } while (k != p_stage);
+            p_seg = n_seg;
+            lost = true;
+            break;
+          }
           phases ^= 1u << stage;
         }
         if (++stage == S) stage = 0;
@@ -531,6 +542,7 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
+          if (lost) l[t][z] = NAN;                       // incomplete, and looks it
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) l[t][z] += __shfl_xor_sync(0xffffffffu, l[t][z], x);
           float *p = meet + ((w * NT + t) * 8 + 2 * c + z) * G::PITCH + G::VB * r;

@@ -55,3 +55,30 @@ def test_rows_of_a_prompt_whose_wait_runs_out_are_not_a_numbers(fmt, d, waits):
         assert (out[n:] == 7.0).all() and (lse[n:] == 7.0).all()
         again, again_lse = attend(b.pages, b.table_dev, lengths, rows, q, causal=causal)         # the next call is as if nothing had been
         assert torch.equal(again, want) and torch.equal(again_lse, want_lse) and b.status.item() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,hq,heads,d", [(E4M3, 32, 8, 128), (INT8, 8, 4, 64)])
+@pytest.mark.parametrize("rows,wide", [(1, False), (1, True), (4, False), (4, True)])
+def test_rows_of_a_copy_that_does_not_arrive_are_not_a_numbers(fmt, hq, heads, d, rows, wide):
+    """In clusters and on the line, where a CTA goes on to other heads: every row that sees a token lacks one.  One that sees none is complete
+    unless it shares a CTA with those."""
+    lengths = [900, 0, 5000 if wide else 300, 17]
+    b = filled(fmt, heads, 64, d, lengths, seed=5)
+    q = randn(4 * rows + 2, hq, d, seed=9, scale=2.0).to(DEV)
+    if wide:
+        table = torch.full((4, 1 << 16), 10 ** 9, dtype=torch.int32, device=DEV)                 # never looked at
+        table[:, :b.table_dev.shape[1]] = b.table_dev
+        b.table_dev = table
+    n = 4 * rows
+    sees = torch.tensor([s != 1 for s in range(4) for _ in range(rows)], device=DEV)
+    want, want_lse = attend(b.pages, b.table_dev, lengths, [rows] * 4, q, max_rows=rows)
+    assert want[:n].isfinite().all()
+    out, lse, status = lost(b, lengths, [rows] * 4, q, wnw.WNW_DEBUG_WAIT_GRANULE, max_rows=rows)
+    assert status == wnw.WNW_PAGES_TIMEOUT
+    gone = out[:n].isnan().all(-1)
+    assert torch.equal(gone, lse[:n].isnan()) and gone[sees].all()
+    assert (out[:n][~gone] == 0).all() and lse[:n][~gone].isneginf().all()
+    assert (out[n:] == 7.0).all() and (lse[n:] == 7.0).all()
+    again, again_lse = attend(b.pages, b.table_dev, lengths, [rows] * 4, q, max_rows=rows)
+    assert torch.equal(again, want) and torch.equal(again_lse, want_lse) and b.status.item() == 0
