@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(Geo<D, NT>::THREADS, 1) wnw_pages_attend_kerne
     const uint32_t count = a.lose & WNW_DEBUG_WAIT_GRANULE ? 2 : 1;     // (an arrival that nothing makes, where a test asks for copies that do not arrive)
     for (int k = 0; k < S; ++k) asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"((uint32_t)__cvta_generic_to_shared(bars + w * S + k)), "r"(count) : "memory");
     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-    asm volatile("prefetch.tensormap [%0];\n" ::"l"(&map) : "memory");
+    if (pv.n_pages) asm volatile("prefetch.tensormap [%0];\n" ::"l"(&map) : "memory");   // (a store of no pages has no map)
   }
   __syncwarp();
   if (!CLUSTER) pg_let_next_start();
