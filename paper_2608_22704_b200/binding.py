@@ -660,7 +660,8 @@ def wnw_debug_pages_lose(waits: int) -> None:
 def wnw_pages_attend(pages, page_table, lengths, row_starts, q, out, workspace, lse=None, causal=True, softmax_scale=0.0, max_rows=0,
                      stream=None):
     """q, out: [n_rows, n_q_heads, head_dim] bf16 or fp16; lse: None or float32 [n_rows, n_q_heads]; workspace: a CUDA tensor of
-    wnw_pages_attend_workspace bytes."""
+    wnw_pages_attend_workspace bytes.  max_rows: the most rows of a sequence; give it where it is known, for 0 counts as n_rows and
+    the work is cut for it."""
     dtypes, _, float32, raw_stream, _, _, _, call = _calls or _prepare_calls()
     what, device, shape, dtype = "wnw_pages_attend", pages.device, q.shape, q.dtype
     if len(shape) != 3 or shape[2] != pages.head_dim:

@@ -127,8 +127,8 @@ template <typename T> __device__ __forceinline__ void turn_unit(bool neighbours,
 
 // CTA: (KV head and K|V; pages of a sequence, one at a time; sequence).  Where keys are turned, `heads` heads of K share a CTA: its threads
 // keep the angles of their pieces' pairs from one to the next.  A thread keeps its N pieces of eight elements in registers from the
-// one pass over the rows to the codes; 1536 threads an SM instead of 1024
-// write 194 MB of rows in 53 us instead of 59 (bytes alone: 44).
+// one pass over the rows to the codes: 194 MB of rows in 55 to 58 us (bytes alone: 44).  (1536 threads an SM instead of 1024 took 53 instead of 59
+// when it was done.)
 template <typename T, int D, int FMT, int N, int THREADS, bool TURN>
 __global__ void __launch_bounds__(THREADS, (TURN && N == 8 ? 512 : TURN || N == 8 ? 1024 : 1536) / THREADS) wnw_pages_write_kernel(const __grid_constant__ WriteArgs a) {
   constexpr int PPR = D / 8;                           // pieces of a row
@@ -339,7 +339,8 @@ template <typename T, int D, int FMT, bool TURN> cudaError_t launch_write(const 
 }
 // Angles are the larger part of turning a key, and the same for all heads, so that several share a CTA, and the values go by themselves (the
 // kernel that turns has registers for fewer threads): 30000 tokens of 8 heads of 128, a head a CTA 91 us, four 78, the values apart 66, 1024
-// threads an SM 57; wnw_rotate and then a write take 60.  A few new rows are done soonest a head a CTA, values in the same launch.
+// threads an SM 57 (53 in e4m3; bytes alone: 28); wnw_rotate and then a write take 60 (58).  A few new rows are done soonest a head a CTA,
+// values in the same launch.
 template <typename T, int D, int FMT> cudaError_t launch_write(WriteArgs &a, int max_rows, dim3 grid, cudaStream_t st) {
   a.values_only = false;
   if (!a.rot.n_pairs) { grid.x = 2 * a.pv.H; return launch_write<T, D, FMT, false>(a, grid, st); }

@@ -11,16 +11,16 @@
 // to eight query rows fills an operand.  The order of the contracted index is free as long as both operands agree, so every lane keeps
 // to 16 bytes of a row at a time.  A granule comes as one TMA copy (K and V rows, swizzled so that no bank conflicts arise) into the
 // warp's own ring in shared memory.  (Copies of 16 bytes a lane, cp.async, moved 5.0 TB/s however many warps and stages there were;
-// these 6.6.)  Codes become fp16 exactly (e4m3 has 4 significant bits, int8 8); the query is scaled by a power of two to the top of
-// fp16's range (exact but for elements 2^-32 of its largest); weights are fp16 against a reference within 2^8 of the largest.  Sums,
-// maxima and accumulators are fp32.
+// these 6.4 then.)  Codes become fp16 exactly (e4m3 has 4 significant bits, int8 8); the query is scaled by a power of two to the top of
+// fp16's range (elements below 2^-31 of its largest lose bits, below 2^-39 they are zero); weights are fp16 against a reference within 2^8
+// of the largest.  Sums, maxima and accumulators are fp32.
 //
 // The scales 2^eV sit inside the sum over tokens.  A second reference M, the maximum of s + eV in log2, carries them: weights enter the
 // product as 2^(s + eV - M), the denominator as 2^(s - m), and out = product * 2^(M - m) / denominator.  No spread of scales over the
 // pages can push the weights that matter out of fp16's range.
 //
-// 16 sequences of 50001 tokens, 8 KV heads of 128, e4m3: 248 us, 6.6 TB/s (the measured copy rate is 6.5).  Some 10 us of a call on the line go
-// into laying it out, its first copies, and the join: 32 sequences of up to 7500 tokens, int8, 332 MB, take 74 us.
+// 16 sequences of 50001 tokens, 8 KV heads of 128, e4m3: 245 to 282 us from box to box, 5.8 to 6.7 TB/s (the measured copy rate is 6.5).  Some 10 us
+// of a call on the line go into laying it out, its first copies, and the join; 32 sequences of up to 7500 tokens, 332 MB, take 74 us in int8, 70 in e4m3.
 #include <cuda.h>
 
 #include <algorithm>
@@ -799,7 +799,7 @@ template <int D, int FMT> cudaError_t launch(const AttendArgs &a, const CUtensor
 }
 
 // CTAs of a cluster for each head of each sequence, all at once on the GPU; 0: the line.  The line is even whatever the lengths, but lays
-// itself out and joins its heads in a second launch; a cluster does neither.  us a call in clusters / on the line, e4m3, 128 elements: 8 KV
+// itself out and joins its heads in a second launch; a cluster does neither.  us a call in clusters / on the line when the rule was made, e4m3, 128 elements: 8 KV
 // heads of 1000 tokens 6.8 / 11.8, of 3064 8.2 / 10.4, of 15000 16.0 / 17.1, of 30000 26.3 / 23.4; int8, 64 heads of 1000 8.7 / 13.5, of 3000
 // 15.2 / 17.5, of 7500 29.3 / 26.4; 128 heads of 3000 24.5 / 25.9.  What a CTA may have to read decides: the table's width says how much, and
 // the tiles of query tokens how often.
@@ -879,9 +879,10 @@ extern "C" wnw_status_t wnw_pages_attend(const wnw_pages_attend_t *call) {
   a.part_row = (PartRow *)((char *)workspace_dev + rows_at);
   a.part_head = (PartHead *)((char *)workspace_dev + heads_at);
   const int max_rows = batch->max_rows > 0 ? std::min(batch->max_rows, batch->n_rows) : batch->n_rows, d = pages->head_dim;
-  // Rows of a KV head that one call of a sequence brings: up to 16 in a pass over the codes, more in passes (the second from L2), from 49 on
-  // by the tensor cores' tiles of 128.  us, passes / tiles: 32 sequences of 7500 tokens, 8 KV heads of 128, int8, 20 rows 139 / 264, 32 rows
-  // 172 / 265, 48 rows 252 / 270, 64 rows 272 / 272; one of 3064, e4m3, 32 rows 20.7 / 26.4, 48 rows 30.5 / 28.3, 64 rows 40 / 30.
+  // Rows of a KV head that one call of a sequence brings: up to 16 in a pass over the codes, more in passes (the later ones from L2 as far as the
+  // codes fit), from 49 on by the tensor cores' tiles of 128.  us, passes / tiles, 8 KV heads of 128: 32 sequences of up to 7500 tokens and
+  // up to so many rows, int8, 20 rows 133 / 251, 32 rows 167 / 252, 48 rows 242 / 254; all of the full length and rows, 20 rows 252 / 327,
+  // 32 rows 254 / 329, 48 rows 376 / 330; one of 3064, e4m3, 20 rows 20.2 / 23.1, 32 rows 21.4 / 24.0, 48 rows 31.3 / 24.2.
   const bool prompt = (long long)max_rows * a.g > 48;
   const int nt = (long long)max_rows * a.g <= 8 ? 1 : 2;
   a.blocks = prompt ? PP_BLOCKS : 1;
