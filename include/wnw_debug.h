@@ -48,9 +48,9 @@ typedef enum {
 wnw_status_t wnw_debug_get_layer_cut(wnw_cache_t *cache, int32_t layer, int32_t cut[3]);
 
 /* Test hook for wnw_pages_attend's bounded waits: in the calls of the process that follow (captured ones as they are captured), waits of
- * these kinds are for something that never happens, and waits give up after 2^20 SM clocks.  A CTA whose wait runs out touches nothing of
- * what stands behind it, sets WNW_PAGES_TIMEOUT in the store's status word, lets what it has under way finish and writes not-a-numbers
- * to the rows that it has not finished.  0: none, as at the start.  Not for production use. */
+ * these kinds are for something that never happens, and waits give up after 2^20 SM clocks.  A CTA whose wait runs out sets
+ * WNW_PAGES_TIMEOUT in the store's status word, starts nothing new, lets what it has under way come to rest before it touches anything
+ * else, and writes not-a-numbers to the rows that it has not finished.  0: none, as at the start.  Not for production use. */
 typedef enum {
   WNW_DEBUG_WAIT_K_FREE = 1,     /* of many rows: room for a tile of K as fp16 */
   WNW_DEBUG_WAIT_V_FREE = 2,     /* ... of V */

@@ -1,5 +1,5 @@
 """What a wait of wnw_pages_attend that runs out leaves behind.  The debug hook has kernels wait for what never happens, for half a
-millisecond; nothing of what stands behind such a wait is touched, so no GPU is put at risk."""
+millisecond; a kernel starts nothing behind such a wait and goes on only when what it has under way is at rest, so no GPU is put at risk."""
 import pytest
 import torch
 
